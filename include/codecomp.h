@@ -264,6 +264,117 @@ int cc_ppl_chunk_scores(cc_ctx* ctx, const void* logits, int32_t logits_dtype, i
 int cc_select_chunks(cc_ctx* ctx, const float* score, int32_t num_chunks, int32_t k,
                      int32_t* chosen, void* stream);
 
+/* ---- after the compression: new tokens on a paged cache -----------------------------------
+ *
+ * The retained rows sit in pages (cc_compact_kv, cc_compress_layer with page_size > 0); a request goes on by
+ * rotating the queries and keys of its new tokens, appending keys and values to the cache
+ * (cc_rope_append) and attending over the cache (cc_paged_attention), one token at a time or a chunk of
+ * tokens at once; cc_fork_pages lets several requests go on from one cache.  All three take one descriptor.
+ *
+ * Layout.  Sequence s has n_s = kv_lens[s] tokens in the cache, its new_lens[s] = T_s new ones last: new token t
+ * of the sequence is slot n_s - T_s + t.  new_off[s] = sum of earlier T_s.
+ *    q_new, q, out     bf16 [sum T_s][H_q][d]    new token t of sequence s is row new_off[s] + t
+ *    k_new, v_new      bf16 [sum T_s][H_kv][d]
+ *    lse               f32  [sum T_s][H_q]       natural log of the sum of exp of the scaled logits
+ *    positions         i32  [sum T_s]
+ *    k, v              bf16 page pool [pool_pages * page_size][H_kv][d]: slot j of sequence s is row
+ *                      page_table[s][j / page_size] * page_size + j % page_size.  Sequences may share pages.
+ * Only the first ceil(n_s / page_size) entries of a row of the page table are read.  A page id outside
+ * [0, pool_pages) is skipped and flagged (CC_ERR_DEVICE_FLAG in the status word).
+ *
+ * Lengths on the device.  With dev_kv_lens, n_s is read there when the work runs and kv_lens holds an upper
+ * bound of each, so that a captured graph can be replayed while its sequences grow; a value outside
+ * [0, kv_lens[s]] is clamped and flagged.  Work is shared out by the lengths found.
+ *
+ * These calls run on the context's device, whichever is current. */
+
+#define CC_ROPE_PLAIN  0   /* f_i = base^(-2i / dims) */
+#define CC_ROPE_LINEAR 1   /* f_i / factor: positions divided by the factor */
+#define CC_ROPE_BASE   2   /* base stretched to base * factor^(dims / (dims - 2)) */
+#define CC_ROPE_BANDS  3   /* by turns over the original length, r_i = original * f_i / (2 pi): f_i / factor where
+                              r_i <= low, f_i where r_i >= high, between them (1 - g) f_i / factor + g f_i with
+                              g = (r_i - low) / (high - low) */
+#define CC_ROPE_GIVEN  4   /* f_i = inv_freq[i] */
+
+typedef struct cc_rope_params {
+  int32_t kind;             /* CC_ROPE_* */
+  int32_t dims;             /* rotated channels of a head: a multiple of 16, 16..128 */
+  double  base;             /* > 1 */
+  double  factor;           /* >= 1; LINEAR, BASE, BANDS */
+  double  low, high;        /* BANDS: 0 < low < high */
+  double  original;         /* BANDS: context length before scaling, > 0 */
+  const double* inv_freq;   /* GIVEN: HOST [dims / 2], finite and >= 0, radians per position */
+} cc_rope_params;
+
+/* Host call: the rotation frequencies as cc_cache_desc takes them, freqs[i] = the fraction of f_i / (2 pi) (turns
+ * per position) in units of 2^-64, for i < dims / 2.  A position times such a word, modulo 2^64, is the angle's
+ * place on the circle without any loss, however far the position. */
+int cc_rope_freqs(const cc_rope_params* p, uint64_t* freqs);
+
+typedef struct cc_cache_desc {
+  int32_t n_heads_q;          /* H_q, a multiple of n_heads_kv, at most 128 times it */
+  int32_t n_heads_kv;         /* H_kv */
+  int32_t head_dim;           /* must be 128 */
+  int32_t dtype;              /* CC_BF16 */
+  int32_t num_seqs;           /* 1 .. CC_MAX_SEQS */
+  int32_t page_size;          /* 8, 16, 32, 64 or 128 tokens */
+  int32_t pool_pages;         /* pages of the pool */
+  int32_t page_table_stride;  /* row length of page_table, at least ceil(n_s / page_size) */
+  const int32_t* page_table;  /* DEVICE [num_seqs][page_table_stride] */
+  const int32_t* kv_lens;     /* HOST [num_seqs] */
+  const int32_t* new_lens;    /* HOST [num_seqs]; NULL: one new token each */
+  const int32_t* dev_kv_lens; /* DEVICE [num_seqs] or NULL */
+  int64_t q_new_stride_tok, q_new_stride_head;    /* q_new of cc_rope_append; strides in elements, 0 = dense */
+  int64_t kv_new_stride_tok, kv_new_stride_head;  /* k_new and v_new */
+  int64_t q_stride_tok, q_stride_head;            /* q: written by cc_rope_append, read by cc_paged_attention */
+  int64_t kv_stride_tok, kv_stride_head;          /* k and v */
+  int64_t out_stride_tok, out_stride_head;        /* out */
+  int32_t causal;             /* 1: new token t attends to slots up to its own; 0: to all n_s (the states of an
+                                 encoder, a prompt's chunks without the query's own tokens) */
+  float   scale;              /* logits are scale * q . k; 0 = 1 / sqrt(head_dim) */
+  int32_t rope_dims;          /* channels that cc_rope_append rotates: a multiple of 16 up to 128; 0 = none */
+  int32_t rope_interleaved;   /* pairs of channels: 0 = (i, i + rope_dims / 2), 1 = (2i, 2i + 1) */
+  float   rope_scale;         /* factor of the rotated values (long-context scalings); 0 = 1 */
+  const uint64_t* rope_freqs; /* HOST [rope_dims / 2], from cc_rope_freqs */
+} cc_cache_desc;
+
+/* Rotary positions and append.  For every new token with position p, every head of q_new and k_new, and every pair
+ * (x, y) of the first rope_dims channels, with angle a = p * f_i:
+ *   (x, y) -> rope_scale * (x cos a - y sin a, x sin a + y cos a),
+ * the other channels and v_new are copied.  Rotated queries go to q (which may be q_new itself, with the same
+ * strides), rotated keys and the values to the tokens' slots of the cache; nothing else of the pool is written.
+ * Arithmetic in f32, one rounding.  positions NULL: the slot is the position (an uncompressed cache).  q_new NULL:
+ * keys and values only (q unused).  k_new NULL: queries only (k_new, v_new, k, v unused; slots need no pages).
+ * Needs n_s >= T_s for every sequence where keys are appended (a value of dev_kv_lens below T_s is flagged, and
+ * tokens without a slot are not appended).  Sequences that append to one shared page race: fork first. */
+int cc_rope_append(cc_ctx* ctx, const cc_cache_desc* desc, const void* q_new, const void* k_new,
+                   const void* v_new, const int32_t* positions, void* q, void* k, void* v, void* stream);
+
+/* Bytes of device workspace (256-byte aligned) that cc_paged_attention needs.  0: invalid descriptor. */
+size_t cc_attention_workspace_bytes(const cc_ctx* ctx, const cc_cache_desc* desc);
+
+/* Attention of the new tokens over the cache.  For new token t of sequence s and query head h, with the KV head
+ * h / (H_q / H_kv), over the slots j that it attends to (all, or those up to n_s - T_s + t):
+ *   out = sum_j softmax_j(scale * q . k_j) v_j,   lse = log sum_j exp(scale * q . k_j).
+ * A token that attends to no slot gets out = 0 and lse = -inf.  lse may be NULL.  bf16 operands, f32 products, sums
+ * and softmax, probabilities rounded to bf16 for the product with v, one rounding of the result.  Rows of k and v
+ * beyond n_s are never used, whatever they hold.  out must not overlap q, k or v. */
+int cc_paged_attention(cc_ctx* ctx, const cc_cache_desc* desc, const void* q, const void* k,
+                       const void* v, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
+
+/* Forks sequences: child f continues sequence parents[f].  Its row of child_table names the parent's full pages
+ * (shared from now on) and, where the parent's last page is not full, the fresh page free_pages[f], which receives
+ * the rows of that page up to n_s in every layer; the remaining entries become -1.  free_pages[f] of a child
+ * whose parent ends with a full page is not used.  k, v: HOST arrays of n_layers device pointers (page pools of
+ * one geometry; the page table is common to the layers).  parents: HOST [n_children], n_children at most
+ * CC_MAX_CHILDREN.  child_table: device i32 [n_children][child_table_stride], child_table_stride at least the
+ * pages of every parent; it may lie in the array of page_table as long as no child's row is a parent's.
+ * free_pages: device i32 [n_children], different pages that no sequence uses. */
+#define CC_MAX_CHILDREN 256
+int cc_fork_pages(cc_ctx* ctx, const cc_cache_desc* desc, int32_t n_layers, void* const* k, void* const* v,
+                  const int32_t* parents, int32_t n_children, int32_t* child_table,
+                  int32_t child_table_stride, const int32_t* free_pages, void* stream);
+
 /* ---- host-side planning (no GPU work, no context; all pointers are HOST memory) ----------- */
 
 /* Section 4.3 "Structure-Aware Budget Allocation", with the appendix's multiplier range

@@ -29,13 +29,16 @@ CC_MODE_BF16, CC_MODE_FP32 = 0, 1
 CC_POOL_NONE, CC_POOL_MAX, CC_POOL_AVG = 0, 1, 2
 CC_MAX_SEQS = 64
 CC_FILL_ATTENTION, CC_FILL_NEAREST = 0, 1
+CC_ROPE_PLAIN, CC_ROPE_LINEAR, CC_ROPE_BASE, CC_ROPE_BANDS, CC_ROPE_GIVEN = 0, 1, 2, 3, 4
+CC_MAX_CHILDREN = 256
 
 EXPORTS = ("cc_create", "cc_destroy", "cc_status_string", "cc_last_error", "cc_poll_status",
            "cc_workspace_bytes", "cc_score_window", "cc_fuse_prior_pool", "cc_topk_select",
            "cc_compact_kv", "cc_compress_layer", "cc_workspace_views", "cc_topk_select_static",
            "cc_structural_score", "cc_plan_budgets", "cc_select_spans", "cc_ppl_chunk_scores",
            "cc_select_chunks", "cc_exp_rate_probe", "cc_compress_layers",
-           "cc_layers_workspace_bytes")
+           "cc_layers_workspace_bytes", "cc_rope_freqs", "cc_rope_append", "cc_attention_workspace_bytes",
+           "cc_paged_attention", "cc_fork_pages")
 CC_STATIC_SELECT_MAX_ITEMS = 1 << 20
 
 
@@ -65,13 +68,37 @@ class cc_layer_desc(C.Structure):
     ]
 
 
+class cc_cache_desc(C.Structure):
+    _fields_ = [
+        ("n_heads_q", C.c_int32), ("n_heads_kv", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32),
+        ("num_seqs", C.c_int32), ("page_size", C.c_int32), ("pool_pages", C.c_int32), ("page_table_stride", C.c_int32),
+        ("page_table", C.c_void_p),
+        ("kv_lens", C.POINTER(C.c_int32)), ("new_lens", C.POINTER(C.c_int32)), ("dev_kv_lens", C.c_void_p),
+        ("q_new_stride_tok", C.c_int64), ("q_new_stride_head", C.c_int64),
+        ("kv_new_stride_tok", C.c_int64), ("kv_new_stride_head", C.c_int64),
+        ("q_stride_tok", C.c_int64), ("q_stride_head", C.c_int64),
+        ("kv_stride_tok", C.c_int64), ("kv_stride_head", C.c_int64),
+        ("out_stride_tok", C.c_int64), ("out_stride_head", C.c_int64),
+        ("causal", C.c_int32), ("scale", C.c_float),
+        ("rope_dims", C.c_int32), ("rope_interleaved", C.c_int32), ("rope_scale", C.c_float),
+        ("rope_freqs", C.POINTER(C.c_uint64)),
+    ]
+
+
+class cc_rope_params(C.Structure):
+    _fields_ = [("kind", C.c_int32), ("dims", C.c_int32), ("base", C.c_double), ("factor", C.c_double),
+                ("low", C.c_double), ("high", C.c_double), ("original", C.c_double),
+                ("inv_freq", C.POINTER(C.c_double))]
+
+
 _LIB = None
 _BIND = None          # the extension's bind(name, address, spec): see csrc/py_call.cpp
 # arguments of the entry points that are called through it
 _SPEC = {"cc_score_window": b"iittttwi", "cc_fuse_prior_pool": b"iittti", "cc_topk_select": b"iittttwi",
          "cc_topk_select_static": b"iitttti", "cc_compact_kv": b"iippttttti",
          "cc_compress_layer": b"iittptttttttwi", "cc_compress_layers": b"iiiLLLtLLLLLLwi",
-         "cc_ppl_chunk_scores": b"itiiiiiittti", "cc_select_chunks": b"itiiti"}
+         "cc_ppl_chunk_scores": b"itiiiiiittti", "cc_select_chunks": b"itiiti",
+         "cc_rope_append": b"iittttttti", "cc_paged_attention": b"iitttttwi", "cc_fork_pages": b"iiiLLiititi"}
 
 
 def load_library(path: Optional[str] = None) -> C.CDLL:
@@ -116,9 +143,17 @@ def load_library(path: Optional[str] = None) -> C.CDLL:
     lib.cc_compress_layer.argtypes = [vp, dp] + [vp] * 10 + [vp, sz, vp]
     lib.cc_exp_rate_probe.argtypes = [vp, C.c_int32, C.c_int32, C.POINTER(C.c_double), vp]
     lib.cc_compress_layers.argtypes = [vp, dp, C.c_int32] + [vp] * 3 + [vp] + [vp] * 6 + [vp, sz, vp]
+    cp = C.POINTER(cc_cache_desc)
+    lib.cc_rope_freqs.argtypes = [C.POINTER(cc_rope_params), C.POINTER(C.c_uint64)]
+    lib.cc_rope_append.argtypes = [vp, cp] + [vp] * 8
+    lib.cc_attention_workspace_bytes.argtypes = [vp, cp]
+    lib.cc_attention_workspace_bytes.restype = sz
+    lib.cc_paged_attention.argtypes = [vp, cp] + [vp] * 6 + [sz, vp]
+    lib.cc_fork_pages.argtypes = [vp, cp, C.c_int32, vp, vp, vp, C.c_int32, vp, C.c_int32, vp, vp]
     lib.cc_workspace_views.argtypes = [vp, dp, vp, C.POINTER(vp), C.POINTER(vp)]
     for name in EXPORTS:
-        if name not in ("cc_status_string", "cc_last_error", "cc_workspace_bytes", "cc_layers_workspace_bytes"):
+        if name not in ("cc_status_string", "cc_last_error", "cc_workspace_bytes", "cc_layers_workspace_bytes",
+                        "cc_attention_workspace_bytes"):
             getattr(lib, name).restype = C.c_int
     if _BIND is None:
         loader = importlib.machinery.ExtensionFileLoader("_cccall", _build.CALL_PATH)
@@ -184,6 +219,16 @@ class Context:
     def workspace(self, desc: "Desc", n_layers: Optional[int] = None) -> torch.Tensor:
         return torch.empty(self.workspace_bytes(desc, n_layers), dtype=torch.uint8,
                            device=f"cuda:{self.device}")
+
+    def cache_workspace_bytes(self, desc: "CacheDesc") -> int:
+        """Bytes of workspace for ``cc_paged_attention``."""
+        n = self.lib.cc_attention_workspace_bytes(self.handle, C.byref(desc.c))
+        if n == 0:
+            raise CodecompError(CC_ERR_INVALID_ARG, self.lib.cc_last_error(self.handle).decode())
+        return int(n)
+
+    def cache_workspace(self, desc: "CacheDesc") -> torch.Tensor:
+        return torch.empty(self.cache_workspace_bytes(desc), dtype=torch.uint8, device=f"cuda:{self.device}")
 
     def poll(self, stream: Optional[int] = None) -> int:
         """Synchronises the stream and returns the device-side status (0 = ok)."""
@@ -264,6 +309,81 @@ class Desc:
         return sum((n + ch - 1) // ch for n in self.lens)
 
 
+class RopePlan:
+    """Rotary frequencies in the form ``cc_rope_append`` takes them (``cc_rope_freqs``): ``dims`` channels of a head,
+    pairs (i, i + dims / 2) or, ``interleaved``, (2i, 2i + 1); ``kind`` is one of CC_ROPE_* (``inv_freq``, radians per
+    position, for CC_ROPE_GIVEN); the rotated values are multiplied by ``attn_factor``."""
+
+    def __init__(self, dims: int = 128, *, base: float = 10000.0, kind: int = CC_ROPE_PLAIN, factor: float = 1.0,
+                 low: float = 1.0, high: float = 4.0, original: float = 8192.0, attn_factor: float = 1.0,
+                 interleaved: bool = False, inv_freq=None, lib=None):
+        lib = lib or load_library()
+        p = cc_rope_params(kind, dims, base, factor, low, high, original)
+        if inv_freq is not None:
+            given = np.ascontiguousarray(inv_freq, dtype=np.float64)
+            if given.shape != (dims // 2,):
+                raise ValueError("inv_freq has one entry per pair of channels")
+            p.inv_freq = given.ctypes.data_as(C.POINTER(C.c_double))
+        self.freqs = np.zeros(max(dims // 2, 1), dtype=np.uint64)
+        rc = lib.cc_rope_freqs(C.byref(p), self.freqs.ctypes.data_as(C.POINTER(C.c_uint64)))
+        if rc != CC_OK:
+            raise CodecompError(rc, lib.cc_status_string(rc).decode())
+        self.dims, self.interleaved, self.attn_factor = dims, interleaved, attn_factor
+
+
+class CacheDesc:
+    """A ``cc_cache_desc`` plus the arrays it points to (kept alive here).  ``kv_lens``: tokens of each sequence in the
+    cache, new ones included; ``new_lens``: new tokens of each (None: one each).  Strides are (token, head) pairs in
+    elements, None = dense."""
+
+    def __init__(self, n_heads_q: int, n_heads_kv: int, kv_lens: Sequence[int], new_lens: Optional[Sequence[int]] = None,
+                 *, page_size: int, page_table: torch.Tensor, pool_pages: int, head_dim: int = 128,
+                 dev_kv_lens: Optional[torch.Tensor] = None, causal: bool = True, scale: float = 0.0,
+                 rope: Optional[RopePlan] = None, q_new_strides=None, kv_new_strides=None, q_strides=None,
+                 kv_strides=None, out_strides=None):
+        c = cc_cache_desc()
+        c.n_heads_q, c.n_heads_kv, c.head_dim, c.dtype = n_heads_q, n_heads_kv, head_dim, CC_BF16
+        lens = np.ascontiguousarray(kv_lens, dtype=np.int32)
+        assert lens.ndim == 1
+        self._keep = [lens, page_table]
+        c.num_seqs = len(lens)
+        c.kv_lens = lens.ctypes.data_as(C.POINTER(C.c_int32))
+        if new_lens is not None:
+            new = np.ascontiguousarray(new_lens, dtype=np.int32)
+            assert new.shape == lens.shape
+            self._keep.append(new)
+            c.new_lens = new.ctypes.data_as(C.POINTER(C.c_int32))
+        assert page_table.dtype == torch.int32 and page_table.is_cuda and page_table.is_contiguous()
+        assert page_table.dim() == 2 and page_table.shape[0] >= c.num_seqs
+        c.page_size, c.pool_pages = page_size, pool_pages
+        c.page_table, c.page_table_stride = page_table.data_ptr(), page_table.shape[1]
+        if dev_kv_lens is not None:
+            assert dev_kv_lens.dtype == torch.int32 and dev_kv_lens.is_cuda and dev_kv_lens.is_contiguous()
+            assert dev_kv_lens.numel() >= c.num_seqs and dev_kv_lens.device == page_table.device
+            self._keep.append(dev_kv_lens)
+            c.dev_kv_lens = dev_kv_lens.data_ptr()
+        c.q_new_stride_tok, c.q_new_stride_head = q_new_strides or (0, 0)
+        c.kv_new_stride_tok, c.kv_new_stride_head = kv_new_strides or (0, 0)
+        c.q_stride_tok, c.q_stride_head = q_strides or (0, 0)
+        c.kv_stride_tok, c.kv_stride_head = kv_strides or (0, 0)
+        c.out_stride_tok, c.out_stride_head = out_strides or (0, 0)
+        c.causal, c.scale = 1 if causal else 0, scale
+        if rope is not None:
+            self._keep.append(rope)
+            c.rope_dims, c.rope_interleaved, c.rope_scale = rope.dims, 1 if rope.interleaved else 0, rope.attn_factor
+            c.rope_freqs = rope.freqs.ctypes.data_as(C.POINTER(C.c_uint64))
+        self.c = c
+
+    @property
+    def lens(self):
+        return [int(x) for x in self._keep[0]]
+
+    @property
+    def n_new(self) -> int:
+        """New tokens of all sequences: rows of the query tensors."""
+        return sum(self.c.new_lens[s] for s in range(self.c.num_seqs)) if self.c.new_lens else self.c.num_seqs
+
+
 # the current stream without a Stream object around it, where this torch has the function
 _CURRENT_RAW = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
@@ -275,6 +395,22 @@ def _raw(stream: Optional[int]) -> int:
     if _CURRENT_RAW is None:
         return torch.cuda.current_stream().cuda_stream
     return _CURRENT_RAW(torch.cuda.current_device())
+
+
+def _raw_on(ctx: "Context", stream: Optional[int]) -> int:
+    """The stream as an integer; None is torch's current stream of the context's device."""
+    if stream is not None:
+        return stream
+    if _CURRENT_RAW is None:
+        return torch.cuda.current_stream(ctx.device).cuda_stream
+    return _CURRENT_RAW(ctx.device)
+
+
+def _check_tensors(ctx: "Context", dtype, *tensors) -> None:
+    """Tensors of a call on a cache: of the given type, on the context's device."""
+    for t in tensors:
+        if t is not None and (t.dtype != dtype or t.get_device() != ctx.device):
+            raise ValueError(f"a {dtype} tensor on cuda:{ctx.device} is needed, got {t.dtype} on {t.device}")
 
 
 def _stream(stream: Optional[int]) -> C.c_void_p:
@@ -419,3 +555,32 @@ def cc_workspace_views(ctx: Context, desc: Desc, ws: torch.Tensor):
     scores = ws[so:so + 4 * hkv * desc.n_tot].view(torch.float32).view(hkv, desc.n_tot)
     fused = ws[fo:fo + 4 * hkv * desc.m_tot].view(torch.float32).view(hkv, desc.m_tot)
     return scores, fused
+
+
+def cc_rope_append(ctx: Context, desc: CacheDesc, q_new, k_new, v_new, positions, q, k, v, stream=None):
+    """Rotates the new tokens' queries into ``q`` and appends rotated keys and values to the cache ``k``, ``v``."""
+    _check_tensors(ctx, torch.bfloat16, q_new, k_new, v_new, q, k, v)
+    _check_tensors(ctx, torch.int32, positions)
+    ctx.call("cc_rope_append", desc, q_new, k_new, v_new, positions, q, k, v, _raw_on(ctx, stream))
+
+
+def cc_paged_attention(ctx: Context, desc: CacheDesc, q, k, v, out, lse=None, ws=None, stream=None):
+    """Attention of the new tokens over the cache into ``out`` (and ``lse``)."""
+    _check_tensors(ctx, torch.bfloat16, q, k, v, out)
+    _check_tensors(ctx, torch.float32, lse)
+    ws = ctx.cache_workspace(desc) if ws is None else ws
+    ctx.call("cc_paged_attention", desc, q, k, v, out, lse, ws, _raw_on(ctx, stream))
+
+
+def cc_fork_pages(ctx: Context, desc: CacheDesc, k_layers, v_layers, parents, child_table, free_pages, stream=None):
+    """Child f continues sequence ``parents[f]`` (host integers): its row of ``child_table`` and, in every layer's pools
+    ``k_layers`` / ``v_layers``, a copy of the parent's last page in ``free_pages[f]`` where that page is not full."""
+    parents = np.ascontiguousarray(parents, dtype=np.int32)
+    _check_tensors(ctx, torch.bfloat16, *k_layers, *v_layers)
+    _check_tensors(ctx, torch.int32, child_table, free_pages)
+    if len(k_layers) != len(v_layers) or free_pages.numel() < len(parents) or child_table.shape[0] < len(parents):
+        raise ValueError("as many value pools as key pools, a fresh page and a row of child_table per child are needed")
+    if not child_table.is_contiguous() or not free_pages.is_contiguous():
+        raise ValueError("child_table and free_pages must be contiguous")
+    ctx.call("cc_fork_pages", desc, len(k_layers), k_layers, v_layers, parents.ctypes.data, len(parents), child_table,
+             child_table.shape[1], free_pages, _raw_on(ctx, stream))

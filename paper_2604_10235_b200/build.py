@@ -15,7 +15,8 @@ LIB_PATH = os.path.join(LIB_DIR, "libcodecomp.so")
 # Python extension that marshals the calls; the suffix names the interpreter it is built for
 CALL_PATH = os.path.join(LIB_DIR, "_cccall" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["api.cu", "score_simt.cu", "score_tc.cu", "fuse_pool.cu", "select.cu", "select_cluster.cu", "compact.cu",
-           "str_score.cu", "planner.cu", "ppl.cu", "exp_probe.cu"]
+           "str_score.cu", "planner.cu", "ppl.cu", "exp_probe.cu", "cache_api.cu", "rope.cu", "fork.cu", "attend.cu",
+           "attend_rows.cu"]
 
 
 def nvcc_path() -> str:

@@ -1,46 +1,17 @@
 // C-ABI layer of libcodecomp: argument checks, batch geometry, workspace carving, launches.
 #include <math.h>
 #include <stddef.h>
-#include <stdarg.h>
 #include <stdio.h>
 #include <string.h>
 
 #include <algorithm>
 #include <new>
 
-#include "cc_internal.cuh"
-
-struct cc_ctx {
-  int device;
-  int sm_count;
-  cc::SelectRoom select_room;
-  cc::DeviceStatus* d_status;
-  cc::DeviceStatus* h_status;   // pinned
-  long long* d_probe;           // scratch of cc_exp_rate_probe: two words per SM
-  void* encode_tiled;           // cuTensorMapEncodeTiled, resolved through the runtime
-  char err[256];
-};
+#include "cc_context.cuh"
 
 namespace {
 
 using namespace cc;
-
-inline size_t align256(size_t x) { return (x + 255) / 256 * 256; }
-
-int fail(cc_ctx* ctx, int code, const char* fmt, ...) __attribute__((format(printf, 3, 4)));
-int fail(cc_ctx* ctx, int code, const char* fmt, ...) {
-  if (ctx) {
-    va_list ap;
-    va_start(ap, fmt);
-    vsnprintf(ctx->err, sizeof(ctx->err), fmt, ap);
-    va_end(ap);
-  }
-  return code;
-}
-
-int cuda_fail(cc_ctx* ctx, cudaError_t e, const char* what) {
-  return fail(ctx, CC_ERR_CUDA, "%s: %s", what, cudaGetErrorString(e));
-}
 
 struct Plan {
   BatchTable bt;
@@ -231,22 +202,6 @@ Group plan_group(const cc_ctx* ctx, const cc_layer_desc* d, const Plan& p, int n
     if (total <= ws_bytes) return Group{layers, p.total, off_ws, total};
   }
   return q;
-}
-
-int check_ws(cc_ctx* ctx, size_t need, void* ws, size_t ws_bytes) {
-  if (!ws) return fail(ctx, CC_ERR_WORKSPACE, "workspace is NULL");
-  if ((uintptr_t)ws % 256) return fail(ctx, CC_ERR_WORKSPACE, "workspace is not 256-byte aligned");
-  if (ws_bytes < need)
-    return fail(ctx, CC_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", ws_bytes, need);
-  return CC_OK;
-}
-
-Launch make_launch(cc_ctx* ctx, void* stream) {
-  Launch L;
-  L.stream = (cudaStream_t)stream;
-  L.status = ctx->d_status;
-  L.sm_count = ctx->sm_count;
-  return L;
 }
 
 int run_score(cc_ctx* ctx, const cc_layer_desc* d, const BatchTable& bt, const Geometry& g, const LayerPtrs& lp,

@@ -90,7 +90,8 @@ struct Entry {
 #define ENTRY(f) {#f, Caller<decltype(&f)>::words, Caller<decltype(&f)>::call}
 const Entry kEntries[] = {ENTRY(cc_score_window), ENTRY(cc_fuse_prior_pool), ENTRY(cc_topk_select),
                           ENTRY(cc_topk_select_static), ENTRY(cc_compact_kv), ENTRY(cc_compress_layer),
-                          ENTRY(cc_compress_layers), ENTRY(cc_ppl_chunk_scores), ENTRY(cc_select_chunks)};
+                          ENTRY(cc_compress_layers), ENTRY(cc_ppl_chunk_scores), ENTRY(cc_select_chunks),
+                          ENTRY(cc_rope_append), ENTRY(cc_paged_attention), ENTRY(cc_fork_pages)};
 #undef ENTRY
 
 struct Bound {                // what a callable holds: an entry point of a loaded library and the spec of its arguments
