@@ -16,7 +16,7 @@ LIB_PATH = os.path.join(LIB_DIR, "libcodecomp.so")
 CALL_PATH = os.path.join(LIB_DIR, "_cccall" + sysconfig.get_config_var("EXT_SUFFIX"))
 SOURCES = ["api.cu", "score_simt.cu", "score_tc.cu", "fuse_pool.cu", "select.cu", "select_cluster.cu", "compact.cu",
            "str_score.cu", "planner.cu", "ppl.cu", "exp_probe.cu", "cache_api.cu", "rope.cu", "fork.cu", "attend.cu",
-           "attend_rows.cu"]
+           "attend_rows.cu", "attend_tc.cu"]
 
 
 def nvcc_path() -> str:

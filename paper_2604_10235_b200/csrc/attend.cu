@@ -73,28 +73,43 @@ attend_join_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, cons
   if (o.lse && lane == 0) o.lse[tok * g.hq + h] = none ? -INFINITY : (top + log2f(total)) * 0.6931471805599453f;
 }
 
+// The launches of a call: sequences with at most 16 query rows per KV head go to the kernel for few rows, the others to the
+// tensor-core kernel (which wants 17 rows and more).
 struct AttendPlan {
   AttendSeqs as;
   int grid;
 };
+struct AttendPlans { AttendPlan rows, tc; };
 
-// The sequences whose blocks have at most `rows` rows.
-AttendPlan plan_rows(const CacheSeqs& cs, const CacheGeom& g, int sm_count) {
-  AttendPlan p = {};
-  AttendSeqs& as = p.as;
-  as.tile_keys = kRowsTile;
-  as.rows = kRowsMost;
-  as.block_tokens = as.tile_tokens = kRowsMost / g.group;
-  as.start_weight = 1;
-  int64_t total = 0;
+AttendPlans plan_attend(const CacheSeqs& cs, const CacheGeom& g, int sm_count) {
+  AttendPlans p = {};
+  AttendSeqs& few = p.rows.as;
+  few.tile_keys = kRowsTile;
+  few.rows = kRowsMost;
+  few.block_tokens = few.tile_tokens = std::max(1, kRowsMost / g.group);
+  few.start_weight = 1;
+  AttendSeqs& many = p.tc.as;
+  many.tile_keys = kTcTile;
+  many.rows = 2 * kTcTile;
+  many.tile_tokens = kTcTile / g.group;
+  many.block_tokens = 2 * many.tile_tokens;
+  many.start_weight = 2;
   for (int s = 0; s < cs.num_seqs; ++s) {
     const int T = cs.new_off[s + 1] - cs.new_off[s];
     if (T == 0) continue;
+    AttendSeqs& as = (int64_t)T * g.group <= kRowsMost ? few : many;
     as.src[as.num++] = (uint8_t)s;
-    const int64_t blocks = (T + as.block_tokens - 1) / as.block_tokens;
-    total += blocks * (as.start_weight + (cs.kv_len[s] + as.tile_keys - 1) / as.tile_keys) * g.hkv;
   }
-  p.grid = (int)std::min<int64_t>(total, sm_count);
+  for (AttendPlan* x : {&p.rows, &p.tc}) {
+    const AttendSeqs& as = x->as;
+    int64_t total = 0;                             // of the weights (attend_weigh), at the longest
+    for (int i = 0; i < as.num; ++i) {
+      const int s = as.src[i];
+      const int64_t blocks = (cs.new_off[s + 1] - cs.new_off[s] + as.block_tokens - 1) / as.block_tokens;
+      total += blocks * (as.start_weight + (cs.kv_len[s] + as.tile_keys - 1) / as.tile_keys) * g.hkv;
+    }
+    x->grid = (int)std::min<int64_t>(total, sm_count);
+  }
   return p;
 }
 
@@ -111,6 +126,17 @@ CUresult encode_pool(EncodeTiledFn encode, const CacheGeom& g, const void* p, in
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
 }
 
+// The tokens of a tile, the heads of a group, half of the channels: rows token * group + head of 128 bytes.
+CUresult encode_queries(EncodeTiledFn encode, const CacheSeqs& cs, const CacheGeom& g, const void* q, int tile_tokens, CUtensorMap* map) {
+  const cuuint32_t estr[3] = {1, 1, 1};
+  const cuuint64_t dims[3] = {(cuuint64_t)kHeadDim, (cuuint64_t)g.hq, (cuuint64_t)cs.new_off[cs.num_seqs]};
+  const cuuint64_t strides[2] = {(cuuint64_t)g.q_head * 2, (cuuint64_t)g.q_tok * 2};
+  const cuuint32_t box[3] = {64, (cuuint32_t)g.group, (cuuint32_t)tile_tokens};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(q), dims, strides, box, estr,
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+}
+
 }  // namespace
 
 cudaError_t launch_attend_join(const Launch& L, const CacheSeqs& cs, const CacheGeom& g, const AttendSeqs& as, const AttendWs& ws,
@@ -121,8 +147,8 @@ cudaError_t launch_attend_join(const Launch& L, const CacheSeqs& cs, const Cache
 }
 
 size_t attend_ws_bytes(const CacheSeqs& cs, const CacheGeom& g, int sm_count) {
-  const AttendPlan p = plan_rows(cs, g, sm_count);
-  return attend_ws_size(p.grid, p.as.rows);
+  const AttendPlans p = plan_attend(cs, g, sm_count);          // one launch after the other uses it
+  return std::max(attend_ws_size(p.rows.grid, p.rows.as.rows), attend_ws_size(p.tc.grid, p.tc.as.rows));
 }
 
 cudaError_t launch_attend(const Launch& L, const CacheSeqs& cs, const CacheGeom& g, const void* q, const void* k, const void* v,
@@ -130,18 +156,29 @@ cudaError_t launch_attend(const Launch& L, const CacheSeqs& cs, const CacheGeom&
   *drv_err = 0;
   const EncodeTiledFn encode = (EncodeTiledFn)encode_fn;
   const AttendOut o = {(uint16_t*)out, lse};
-  const AttendPlan p = plan_rows(cs, g, L.sm_count);
-  if (p.as.num == 0) return cudaSuccess;
-  CUtensorMap k_map, v_map;
-  CUresult r = encode_pool(encode, g, k, p.as.tile_keys, &k_map);
-  if (r == CUDA_SUCCESS) r = encode_pool(encode, g, v, p.as.tile_keys, &v_map);
-  if (r != CUDA_SUCCESS) {
+  const AttendPlans p = plan_attend(cs, g, L.sm_count);
+  CUtensorMap q_map, k_map, v_map;
+  auto pools = [&](int tile_keys) {
+    CUresult r = encode_pool(encode, g, k, tile_keys, &k_map);
+    if (r == CUDA_SUCCESS) r = encode_pool(encode, g, v, tile_keys, &v_map);
     *drv_err = (int)r;
-    return cudaErrorUnknown;
+    return r == CUDA_SUCCESS;
+  };
+  cudaError_t e = cudaSuccess;
+  if (p.tc.as.num > 0) {
+    if (!pools(p.tc.as.tile_keys)) return cudaErrorUnknown;
+    *drv_err = (int)encode_queries(encode, cs, g, q, p.tc.as.tile_tokens, &q_map);
+    if (*drv_err != 0) return cudaErrorUnknown;
+    const AttendWs w = attend_ws(ws, p.tc.grid, p.tc.as.rows);
+    e = launch_attend_tc(L, cs, g, p.tc.as, w, p.tc.grid, o, q_map, k_map, v_map);
+    if (e == cudaSuccess) e = launch_attend_join(L, cs, g, p.tc.as, w, p.tc.grid, o);
   }
-  const AttendWs w = attend_ws(ws, p.grid, p.as.rows);
-  cudaError_t e = launch_attend_rows(L, cs, g, p.as, w, p.grid, o, q, k_map, v_map);
-  if (e == cudaSuccess) e = launch_attend_join(L, cs, g, p.as, w, p.grid, o);
+  if (e == cudaSuccess && p.rows.as.num > 0) {
+    if (!pools(p.rows.as.tile_keys)) return cudaErrorUnknown;
+    const AttendWs w = attend_ws(ws, p.rows.grid, p.rows.as.rows);
+    e = launch_attend_rows(L, cs, g, p.rows.as, w, p.rows.grid, o, q, k_map, v_map);
+    if (e == cudaSuccess) e = launch_attend_join(L, cs, g, p.rows.as, w, p.rows.grid, o);
+  }
   return e;
 }
 

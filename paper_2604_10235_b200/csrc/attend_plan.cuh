@@ -211,6 +211,10 @@ cudaError_t launch_attend_join(const Launch& L, const CacheSeqs& cs, const Cache
 // The kernel for up to 16 rows per block (attend_rows.cu) and the one for blocks of 256 (attend_tc.cu).
 cudaError_t launch_attend_rows(const Launch& L, const CacheSeqs& cs, const CacheGeom& g, const AttendSeqs& as, const AttendWs& ws,
                                int grid, const AttendOut& o, const void* q, const CUtensorMap& k_map, const CUtensorMap& v_map);
+cudaError_t launch_attend_tc(const Launch& L, const CacheSeqs& cs, const CacheGeom& g, const AttendSeqs& as, const AttendWs& ws,
+                             int grid, const AttendOut& o, const CUtensorMap& q_map, const CUtensorMap& k_map,
+                             const CUtensorMap& v_map);
+constexpr int kTcTile = 128;         // keys per tile of attend_tc.cu, and query rows per tile (two tiles a block)
 constexpr int kRowsTile = 64;        // keys per tile of attend_rows.cu
 constexpr int kRowsMost = 16;        // query rows of its blocks
 

@@ -1,0 +1,424 @@
+// Attention of many query rows (chunks of new tokens) over a paged cache, on the tensor cores of sm_100a.
+//
+// A block has two tiles of 128 rows, row = token * group + head of the group, so that K and V of a KV head are read once for
+// its whole group.  Per tile of 128 keys and of rows:
+//
+//   S = Q K^T           tcgen05.mma, both operands in shared memory, S in tensor memory (128 lanes x 128 columns)
+//   P = 2^(S c - ref)   one thread per row: S to registers, maximum, exponentials, P as bf16 back over S
+//   O += P V            tcgen05.mma, P from tensor memory, V as it lies in the cache (channels contiguous: MN-major)
+//
+// Tensor memory holds S and O of both tiles, all 512 columns.  While the four warps of one tile compute exponentials the tensor
+// core works on the other tile.  The reference of a row's exponentials is replaced, and its O scaled in tensor memory, only
+// when a logit exceeds it by 2^8; P is at most 2^8, which bf16 holds as well as 1.
+//
+// Roles (320 threads, one CTA per SM): warps 0-3 and 4-7 the softmax of the two tiles, warp 8 the copies (Q once per
+// problem, K and V by turns through a ring of five stages of 32 KB, a copy per page), warp 9 the products.
+#include <cuda_bf16.h>
+
+#include "attend_plan.cuh"
+#include "exp2_poly.cuh"
+#include "tc_ptx.cuh"
+
+namespace cc {
+
+namespace {
+
+constexpr int kThreads = 320;
+constexpr int kTmaWarp = 8, kMmaWarp = 9;
+constexpr int kStages = 5;
+constexpr uint32_t kTileBytes = kTcTile * kHeadDim * 2;        // of K, of V, or of one tile of Q
+constexpr float kSlack = 8.0f;                                 // log2 of how far a logit may lie above the reference
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+struct Shared {
+  AttendShare share;
+  uint64_t full[kStages], empty[kStages];
+  uint64_t q_full, q_empty;
+  uint64_t s_full[2], p_full[2], o_full[2], o_empty[2];        // per tile of the block
+  uint32_t tmem_base;
+  int abort_flag;
+};
+constexpr size_t kSmem = 1024 + (size_t)(kStages + 2) * kTileBytes + sizeof(Shared);
+static_assert(kSmem <= kSmemPerCta, "shared memory of a CTA");
+
+__device__ __forceinline__ float max3_nan(float a, float b, float c) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+
+__global__ void __launch_bounds__(kThreads, 1)
+attend_tc_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, const __grid_constant__ AttendSeqs as,
+                 const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
+                 const __grid_constant__ CUtensorMap v_map, const AttendOut o, const AttendWs ws, DeviceStatus* status) {
+  extern __shared__ uint8_t dyn[];
+  uint8_t* q_smem = dyn + ((1024u - (smem_u32(dyn) & 1023u)) & 1023u);
+  uint8_t* ring = q_smem + 2 * kTileBytes;
+  Shared* sh = reinterpret_cast<Shared*>(ring + (size_t)kStages * kTileBytes);
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  pdl_launch_dependents();
+  if (warp == kMmaWarp) {
+    if (lane < kStages) {
+      mbar_init(smem_u32(&sh->full[lane]), 1);
+      mbar_init(smem_u32(&sh->empty[lane]), 1);
+    }
+    if (lane < 2) {
+      mbar_init(smem_u32(&sh->s_full[lane]), 1);
+      mbar_init(smem_u32(&sh->p_full[lane]), 4);
+      mbar_init(smem_u32(&sh->o_full[lane]), 1);
+      mbar_init(smem_u32(&sh->o_empty[lane]), 4);
+    }
+    if (lane == 0) {
+      mbar_init(smem_u32(&sh->q_full), 1);
+      mbar_init(smem_u32(&sh->q_empty), 1);
+      sh->abort_flag = 0;
+    }
+    fence_barrier_init();
+    __syncwarp();
+    tmem_alloc(smem_u32(&sh->tmem_base), 512);
+    tmem_relinquish();
+  }
+  pdl_wait();
+  attend_weigh(cs, g, as, &sh->share, status);
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const int workers = attend_workers(as, &sh->share, g.hkv, gridDim.x);
+  if (warp < 2) {
+    const Place p = attend_place(cs, g, as, &sh->share, blockIdx.x + warp, workers);
+    if (lane == 0) {
+      if (warp == 0) {
+        sh->share.from = p;
+        ws.place[blockIdx.x] = blockIdx.x < workers ? p : Place{0, 0, 0, -1};
+      } else {
+        sh->share.to = p;
+      }
+    }
+  }
+  __syncthreads();
+  const uint32_t tmem = __shfl_sync(0xffffffffu, sh->tmem_base, 0);
+  const BoundedWait pipe = {&sh->abort_flag, &status->code};
+  auto wait = [&](uint64_t* bar, uint32_t parity, int where) { return bounded_wait(pipe, bar, parity, CC_ERR_TIMEOUT, where); };
+  AttendWalk w;
+
+  if (warp == kTmaWarp) {
+    // ---------------------------------------------------------------- copies
+    const int span = 1 << g.page_shift, copies = kTcTile >> g.page_shift;
+    const uint32_t copy_bytes = (uint32_t)span * kHeadDim * 2;
+    const uint32_t q_bytes = (uint32_t)(as.tile_tokens * g.group) * 128u;        // of one half of the channels of a tile
+    const bool elected = elect_one();
+    int stage = 0;
+    uint32_t phase = 0, q_phase = 0;
+    bool ok = true;
+    for (bool more = w.first(cs, g, as, &sh->share); more && ok; more = w.next(cs, g, as, &sh->share)) {
+      const int limit = attend_limit(cs, g, as, w.s, w.n, w.at.b);
+      const int32_t* table = g.table + (int64_t)w.s * g.table_stride;
+      const int tok0 = w.at.b * as.block_tokens;
+      const bool second = w.T - tok0 > as.tile_tokens;
+      for (int t = w.t0; t < w.t1 && ok; ++t) {
+        const int key = t * kTcTile + lane * span;             // first key of this lane's copy
+        const bool mine = lane < copies && key < limit;
+        int page = -1;
+        if (mine) page = table[key >> g.page_shift];
+        const bool good = mine && page >= 0 && page < g.pool_pages;
+        if (mine && !good) report_error(status, CC_ERR_DEVICE_FLAG, 621);
+        const unsigned mask = __ballot_sync(0xffffffffu, good);
+        const int group8 = (int)(((int64_t)page << g.page_shift) >> 3);
+#pragma unroll 1
+        for (int kv = 0; kv < 2; ++kv) {
+          if (!wait(&sh->empty[stage], phase ^ 1, 81)) { ok = false; break; }
+          const uint32_t fb = smem_u32(&sh->full[stage]);
+          const uint32_t dst = smem_u32(ring) + (uint32_t)stage * kTileBytes;
+          if (elected) mbar_expect_tx(fb, (uint32_t)__popc(mask) * copy_bytes);
+          for (unsigned left = mask; left; left &= left - 1) {
+            const int p = __ffs(left) - 1;
+            const int at = __shfl_sync(0xffffffffu, group8, p);
+            if (elected) tma_load_5d(dst + p * copy_bytes, kv ? &v_map : &k_map, fb, at, w.at.h);
+          }
+          if (++stage == kStages) { stage = 0; phase ^= 1; }
+          if (kv == 0 && t == w.t0) {
+            if (!wait(&sh->q_empty, q_phase ^ 1, 80)) { ok = false; break; }
+            q_phase ^= 1;
+            if (elected) {
+              const uint32_t qb = smem_u32(&sh->q_full);
+              mbar_expect_tx(qb, q_bytes * (second ? 4u : 2u));
+              for (int i = 0; i < (second ? 2 : 1); ++i) {
+                const int tok = cs.new_off[w.s] + tok0 + i * as.tile_tokens;
+                const uint32_t at = smem_u32(q_smem) + (uint32_t)i * kTileBytes;
+                tma_load_3d(at, &q_map, qb, 0, w.at.h * g.group, tok);
+                tma_load_3d(at + kTileBytes / 2, &q_map, qb, 64, w.at.h * g.group, tok);
+              }
+            }
+          }
+        }
+      }
+    }
+  } else if (warp == kMmaWarp) {
+    // ---------------------------------------------------------------- products
+    // Descriptor words: low = start >> 4 | leading offset, high = stride offset >> 4, version 1, 128-byte swizzle.  Q: groups of
+    // eight rows 1 KB apart, the second half of the channels 16 KB on.  K and V: groups of eight keys 2 KB apart, the second half of
+    // the channels 1 KB on (for V that is the leading offset, between 64 channels and the next 64).
+    const uint32_t q_lo = ((smem_u32(q_smem) & 0x3FFFFu) >> 4) | (1u << 16), q_hi = (1024u >> 4) | (1u << 14) | (2u << 29);
+    const uint32_t r_lo = ((smem_u32(ring) & 0x3FFFFu) >> 4), r_hi = (2048u >> 4) | (1u << 14) | (2u << 29);
+    const uint32_t idesc_s = instr_desc(128, 128) | (g.scale < 0.f ? 1u << 13 : 0u);       // of a negative scale -Q is multiplied
+    const uint32_t idesc_o = instr_desc(128, 128) | (1u << 16);                            // V: MN-major
+    const bool elected = elect_one();
+    int stage = 0;
+    uint32_t phase = 0, q_phase = 0, p_phase[2] = {0, 0}, oe_phase[2] = {1, 1};
+    auto next_stage = [&] { if (++stage == kStages) { stage = 0; phase ^= 1; } };
+    auto scores = [&](int i, uint32_t k_lo) {
+      if (elected) {
+#pragma unroll
+        for (int ks = 0; ks < kHeadDim / 16; ++ks) {
+          const uint32_t a = q_lo + (uint32_t)i * (kTileBytes >> 4) + (ks >= 4 ? (kTileBytes / 2) >> 4 : 0u) + (ks & 3) * 2u;
+          const uint32_t b = k_lo + (1u << 16) + (ks >= 4 ? 1024u >> 4 : 0u) + (ks & 3) * 2u;
+          umma(tmem + i * 128, a | ((uint64_t)q_hi << 32), b | ((uint64_t)r_hi << 32), idesc_s, ks > 0);
+        }
+        umma_commit(smem_u32(&sh->s_full[i]));
+      }
+    };
+    auto outputs = [&](int i, uint32_t v_lo, bool accumulate) {
+      if (elected) {
+#pragma unroll
+        for (int ks = 0; ks < kTcTile / 16; ++ks) {
+          const uint32_t b = v_lo + ((1024u >> 4) << 16) + ks * (4096u >> 4);
+          umma_tmem_a(tmem + 256 + i * 128, tmem + i * 128 + ks * 8, b | ((uint64_t)r_hi << 32), idesc_o, accumulate || ks > 0);
+        }
+      }
+    };
+    bool ok = true;
+    for (bool more = w.first(cs, g, as, &sh->share); more && ok; more = w.next(cs, g, as, &sh->share)) {
+      if (w.t0 == w.t1) continue;
+      const bool second = w.T - w.at.b * as.block_tokens > as.tile_tokens;
+      const int tiles = second ? 2 : 1;
+      ok = wait(&sh->full[stage], phase, 82) && wait(&sh->q_full, q_phase, 83);
+      if (!ok) break;
+      q_phase ^= 1;
+      tc_fence_after();
+      for (int i = 0; i < tiles; ++i) scores(i, r_lo + (uint32_t)stage * (kTileBytes >> 4));
+      if (elected) umma_commit(smem_u32(&sh->empty[stage]));
+      if (w.t0 + 1 == w.t1 && elected) umma_commit(smem_u32(&sh->q_empty));
+      next_stage();
+      for (int t = w.t0; t < w.t1 && ok; ++t) {
+        const int v_stage = stage;
+        ok = wait(&sh->full[stage], phase, 84);
+        next_stage();
+        const bool more_keys = t + 1 < w.t1;
+        const int k_stage = stage;
+        for (int i = 0; i < tiles && ok; ++i) {
+          if (t == w.t0) {
+            ok = wait(&sh->o_empty[i], oe_phase[i], 85);
+            oe_phase[i] ^= 1;
+          }
+          ok = ok && wait(&sh->p_full[i], p_phase[i], 86);
+          p_phase[i] ^= 1;
+          if (!ok) break;
+          tc_fence_after();
+          outputs(i, r_lo + (uint32_t)v_stage * (kTileBytes >> 4), t > w.t0);
+          if (i == tiles - 1 && elected) umma_commit(smem_u32(&sh->empty[v_stage]));
+          if (more_keys) {
+            if (i == 0) {
+              ok = wait(&sh->full[k_stage], phase, 87);
+              if (!ok) break;
+              tc_fence_after();
+            }
+            scores(i, r_lo + (uint32_t)k_stage * (kTileBytes >> 4));
+            if (i == tiles - 1 && elected) {
+              umma_commit(smem_u32(&sh->empty[k_stage]));
+              if (t + 2 == w.t1) umma_commit(smem_u32(&sh->q_empty));
+            }
+          } else if (elected) {
+            umma_commit(smem_u32(&sh->o_full[i]));
+          }
+        }
+        if (more_keys) next_stage();
+      }
+    }
+  } else {
+    // ---------------------------------------------------------------- softmax
+    const int i = warp >> 2;                       // tile of the block
+    const int r = (warp & 3) * 32 + lane;          // row of the tile = lane of tensor memory
+    const uint32_t s_addr = tmem + i * 128 + ((uint32_t)((warp & 3) * 32) << 16), o_addr = s_addr + 256;
+    const float c2 = fabsf(g.scale) * kLog2e;
+    const int in_tile = r / g.group;
+    uint32_t s_phase = 0, of_phase = 0;
+    uint32_t entry = 1;                            // of V of the next tile in the order of the ring
+    bool dead = false;
+    for (bool more = w.first(cs, g, as, &sh->share); more; more = w.next(cs, g, as, &sh->share)) {
+      const int tok = w.at.b * as.block_tokens + i * as.tile_tokens + in_tile;       // of the sequence
+      if (w.T - w.at.b * as.block_tokens <= i * as.tile_tokens) {                    // no such tile
+        entry += 2u * (uint32_t)(w.t1 - w.t0);
+        continue;
+      }
+      const bool real = in_tile < as.tile_tokens && tok < w.T;
+      const int lim = real ? (g.causal ? max(0, w.n - w.T + tok + 1) : w.n) : 0;     // keys that the row attends to
+      const int most = attend_limit(cs, g, as, w.s, w.n, w.at.b);
+      const bool idle = !__any_sync(0xffffffffu, real);
+      const int least = __reduce_min_sync(0xffffffffu, real ? lim : 0x7fffffff);
+      float ref = -INFINITY;
+      uint64_t sum[2] = {0ull, 0ull};
+      for (int t = w.t0; t < w.t1; ++t, entry += 2) {
+        if (!dead) dead = !wait(&sh->s_full[i], s_phase, 88 + i);
+        s_phase ^= 1;
+        const int key0 = t * kTcTile;
+        if (!dead && i == 0 && key0 + kTcTile > most) {
+          // rows of V that no row of the block attends to may hold anything: 0 x NaN.  (Both products with V wait for this tile's P.)
+          const int stage = entry % kStages;
+          dead = !wait(&sh->full[stage], (entry / kStages) & 1, 90);
+          for (int e = (most - key0) * 16 + (int)threadIdx.x; e < kTcTile * 16; e += 128)
+            *reinterpret_cast<uint4*>(ring + (size_t)stage * kTileBytes + (e >> 7) * 2048 + ((e >> 3) & 1) * 1024 +
+                                      ((e >> 4) & 7) * 128 + (e & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+          fence_proxy_async();
+        }
+        if (!dead && !idle) {
+          tc_fence_after();
+          uint32_t v[4][32];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + c * 32, v[c]);
+          tmem_wait_ld();
+          const bool edge = key0 + kTcTile > least;
+          if (edge) {
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+              for (int e = 0; e < 32; ++e)
+                if (key0 + c * 32 + e >= lim) v[c][e] = 0xff800000u;
+          }
+          float top[4];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            top[c] = __uint_as_float(v[c][0]);
+#pragma unroll
+            for (int e = 1; e < 31; e += 2) top[c] = max3_nan(top[c], __uint_as_float(v[c][e]), __uint_as_float(v[c][e + 1]));
+            top[c] = max3_nan(top[c], __uint_as_float(v[c][31]), top[c]);
+          }
+          const float high = max3_nan(max3_nan(top[0], top[1], top[2]), top[3], top[3]) * c2;
+          if (__any_sync(0xffffffffu, real && !(high <= ref + kSlack))) {
+            // a row of infinities or of values that are no numbers has no reference: everything becomes NaN
+            float up = max3_nan(ref, high, high);
+            if (up == INFINITY) up = NAN;
+            const float f = ref == -INFINITY ? 0.f : ex2(ref - up);
+            ref = up;
+            const uint64_t f2 = pack2(f, f);
+            sum[0] = mul2(sum[0], f2);
+            sum[1] = mul2(sum[1], f2);
+            if (t > w.t0) {                        // (the products so far are complete: those of S came behind them)
+#pragma unroll 1
+              for (int c = 0; c < 4; ++c) {
+                uint32_t x[32];
+                tmem_ld32(o_addr + c * 32, x);
+                tmem_wait_ld();
+#pragma unroll
+                for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * f);
+                tmem_st32(o_addr + c * 32, x);
+              }
+            }
+          }
+          const float off = ref == -INFINITY ? 0.f : -ref;
+          const uint64_t c22 = pack2(c2, c2), off2 = pack2(off, off);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            uint32_t p[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+              const uint64_t x = fma2(pack2(__uint_as_float(v[c][2 * e]), __uint_as_float(v[c][2 * e + 1])), c22, off2);
+              const uint64_t y = ex2_pair_sfu(x);
+              sum[e & 1] = add2(sum[e & 1], y);
+              float a, b;
+              unpack2(y, a, b);
+              p[e] = pack_bf16(a, b);
+            }
+            tmem_st16(s_addr + c * 16, p);
+          }
+          tmem_wait_st();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sh->p_full[i]));
+      }
+
+      // the rows' outputs
+      if (w.t0 < w.t1) {
+        if (!dead) dead = !wait(&sh->o_full[i], of_phase, 91);
+        of_phase ^= 1;
+        tc_fence_after();
+      }
+      float total;
+      {
+        float a, b;
+        unpack2(add2(sum[0], sum[1]), a, b);
+        total = a + b;
+      }
+      const bool whole = w.whole();
+      const int h = w.at.h * g.group + r - in_tile * g.group;
+      const int64_t row = cs.new_off[w.s] + tok, at = (int64_t)w.slot() * as.rows + i * 128 + r;
+      if (!dead && !idle) {
+        const float inv = lim <= 0 ? 0.f : 1.0f / total;
+        if (real && whole && o.lse) o.lse[row * g.hq + h] = lim <= 0 ? -INFINITY : (ref + log2f(total)) * kLn2;
+        if (real && !whole) ws.stat[at] = make_float2(ref, total);
+#pragma unroll 1
+        for (int c = 0; c < 4; ++c) {
+          uint32_t x[32];
+          if (w.t0 < w.t1) {
+            tmem_ld32(o_addr + c * 32, x);
+            tmem_wait_ld();
+          } else {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) x[e] = 0u;
+          }
+          if (real && whole) {
+            uint4* dst = reinterpret_cast<uint4*>(o.out + row * g.out_tok + h * g.out_head + c * 32);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              uint32_t y[4];
+#pragma unroll
+              for (int k = 0; k < 4; ++k)
+                y[k] = lim <= 0 ? 0u : pack_bf16(__uint_as_float(x[8 * e + 2 * k]) * inv, __uint_as_float(x[8 * e + 2 * k + 1]) * inv);
+              dst[e] = make_uint4(y[0], y[1], y[2], y[3]);
+            }
+          } else if (real) {
+            uint4* dst = reinterpret_cast<uint4*>(ws.out + at * kHeadDim + c * 32);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) dst[e] = make_uint4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
+          }
+          __syncwarp();
+        }
+      }
+      if (w.t0 < w.t1) {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(smem_u32(&sh->o_empty[i]));
+      }
+    }
+  }
+
+  if (*(volatile int*)&sh->abort_flag) {
+    // copies and products still in flight get time to land before shared and tensor memory are released
+#pragma unroll 1
+    for (int k = 0; k < 2000; ++k) __nanosleep(1000);
+  }
+  tc_fence_before();
+  __syncthreads();
+  if (warp == kMmaWarp) {
+    tc_fence_after();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+}  // namespace
+
+cudaError_t launch_attend_tc(const Launch& L, const CacheSeqs& cs, const CacheGeom& g, const AttendSeqs& as, const AttendWs& ws,
+                             int grid, const AttendOut& o, const CUtensorMap& q_map, const CUtensorMap& k_map,
+                             const CUtensorMap& v_map) {
+  const cudaError_t e = allow_smem(attend_tc_kernel);
+  if (e != cudaSuccess) return e;
+  return launch_pdl(attend_tc_kernel, dim3((unsigned)grid), dim3(kThreads), kSmem, L.stream, 1, cs, g, as, q_map, k_map, v_map,
+                    o, ws, L.status);
+}
+
+}  // namespace cc

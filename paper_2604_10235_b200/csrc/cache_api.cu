@@ -31,8 +31,8 @@ int take_desc(cc_ctx* ctx, const cc_cache_desc* d, CacheSeqs* cs, CacheGeom* g) 
   if (!d) return fail(ctx, CC_ERR_INVALID_ARG, "descriptor is NULL");
   if (d->n_heads_q <= 0 || d->n_heads_kv <= 0 || d->n_heads_q % d->n_heads_kv != 0)
     return fail(ctx, CC_ERR_INVALID_ARG, "n_heads_q must be a positive multiple of n_heads_kv");
-  if (d->n_heads_q / d->n_heads_kv > 16 || d->n_heads_q > 65536)
-    return fail(ctx, CC_ERR_UNSUPPORTED, "at most 16 query heads per KV head and 65536 in all");
+  if (d->n_heads_q / d->n_heads_kv > 128 || d->n_heads_q > 65536)
+    return fail(ctx, CC_ERR_UNSUPPORTED, "at most 128 query heads per KV head and 65536 in all");
   if (d->head_dim != kHeadDim) return fail(ctx, CC_ERR_UNSUPPORTED, "head_dim must be 128");
   if (d->dtype != CC_BF16) return fail(ctx, CC_ERR_UNSUPPORTED, "dtype must be CC_BF16");
   if (d->num_seqs < 1 || d->num_seqs > CC_MAX_SEQS)
