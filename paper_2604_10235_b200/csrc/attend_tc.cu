@@ -8,8 +8,13 @@
 //   O += P V            tcgen05.mma, P from tensor memory, V as it lies in the cache (channels contiguous: MN-major)
 //
 // Tensor memory holds S and O of both tiles, all 512 columns.  While the four warps of one tile compute exponentials the tensor
-// core works on the other tile.  The reference of a row's exponentials is replaced, and its O scaled in tensor memory, only
-// when a logit exceeds it by 2^8; P is at most 2^8, which bf16 holds as well as 1.
+// core works on the other tile, and P goes to it in two halves, so that the product with V starts when the first is there.
+//
+// The reference of a row's exponentials need not be its maximum, only near it: P up to 2^24 rounds to bf16 and sums in f32 like
+// P up to 1.  So only the first tile of a row and masked ones look at their maximum beforehand, the others compute with
+// the reference that there is; where the sum of a half tile shows that a logit is far above it (or no number), nothing has been
+// handed over yet, the row's maximum becomes the reference, its O is scaled in tensor memory and the half is computed again.
+// One pair of exponentials in four is evaluated on the FMA pipe (exp2_poly.cuh), for the special-function unit is the fuller one.
 //
 // Roles (320 threads, one CTA per SM): warps 0-3 and 4-7 the softmax of the two tiles, warp 8 the copies (Q once per
 // problem, K and V by turns through a ring of five stages of 32 KB, a copy per page), warp 9 the products.
@@ -27,14 +32,16 @@ constexpr int kThreads = 320;
 constexpr int kTmaWarp = 8, kMmaWarp = 9;
 constexpr int kStages = 5;
 constexpr uint32_t kTileBytes = kTcTile * kHeadDim * 2;        // of K, of V, or of one tile of Q
-constexpr float kSlack = 8.0f;                                 // log2 of how far a logit may lie above the reference
+constexpr float kSlack = 8.0f;                                 // a maximum that far (log2) above the reference replaces it
+constexpr float kMostSum = 16777216.0f;                        // of half a tile
+constexpr float kMostPoly = 100.0f;                            // arguments up to here are computed on the FMA pipe
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 struct Shared {
   AttendShare share;
   uint64_t full[kStages], empty[kStages];
   uint64_t q_full, q_empty;
-  uint64_t s_full[2], p_full[2], o_full[2], o_empty[2];        // per tile of the block
+  uint64_t s_full[2], p_full[2][2], half_done[2], o_full[2], o_empty[2];       // per tile of the block (P: per half of it)
   uint32_t tmem_base;
   int abort_flag;
 };
@@ -50,6 +57,81 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
   return r;
+}
+
+// 2^(v c + off) of 32 values, as bf16 to tensor memory and added to `sum`; POLY: some on the FMA pipe, whose largest value goes
+// into `reach`.
+template <bool POLY>
+__device__ __forceinline__ void exponentials(const uint32_t (&v)[32], uint64_t c2, uint64_t off2, uint32_t p_addr, uint64_t (&sum)[2],
+                                             float& reach) {
+  uint32_t p[16];
+#pragma unroll
+  for (int e = 0; e < 16; ++e) {
+    const float a = __uint_as_float(v[2 * e]), b = __uint_as_float(v[2 * e + 1]);
+    const uint64_t x = fma2(pack2(a, b), c2, off2);
+    const bool poly = POLY && e % 4 == 3;
+    const uint64_t y = poly ? ex2_pair_fma(x) : ex2_pair_sfu(x);
+    if (poly) reach = max3_nan(reach, a, b);
+    sum[e & 1] = add2(sum[e & 1], y);
+    float y0, y1;
+    unpack2(y, y0, y1);
+    p[e] = pack_bf16(y0, y1);
+  }
+  tmem_st16(p_addr, p);
+}
+__device__ __forceinline__ float total_of(const uint64_t (&sum)[2]) {
+  float a, b;
+  unpack2(add2(sum[0], sum[1]), a, b);
+  return a + b;
+}
+__device__ __forceinline__ float max32_nan(const uint32_t (&v)[32]) {
+  float m0 = __uint_as_float(v[0]), m1 = __uint_as_float(v[1]);
+#pragma unroll
+  for (int e = 2; e < 30; e += 4) {
+    m0 = max3_nan(m0, __uint_as_float(v[e]), __uint_as_float(v[e + 1]));
+    m1 = max3_nan(m1, __uint_as_float(v[e + 2]), __uint_as_float(v[e + 3]));
+  }
+  return max3_nan(max3_nan(m0, m1, __uint_as_float(v[30])), __uint_as_float(v[31]), __uint_as_float(v[31]));
+}
+
+__device__ __forceinline__ uint64_t offset_of(float ref) {
+  const float off = ref == -INFINITY ? 0.f : -ref;
+  return pack2(off, off);
+}
+// Whether a row of the warp has a logit far above its reference, or no number.
+__device__ __forceinline__ bool out_of_range(bool real, const uint64_t (&part)[2], float reach, float c2, float ref) {
+  return __any_sync(0xffffffffu, real && !(total_of(part) <= kMostSum && fmaf(reach, c2, -ref) <= kMostPoly));
+}
+// Makes `high` the row's reference where it is far above the one that there is, and scales what the row has: its sum and, with
+// `scale_o`, its O in tensor memory (the products with V so far are complete).
+__device__ __forceinline__ void raise(float high, bool real, float& ref, uint64_t (&sum)[2], bool scale_o, uint32_t o_addr) {
+  if (!__any_sync(0xffffffffu, real && !(high <= ref + kSlack))) return;
+  // a row of infinities or of values that are no numbers has no reference: everything becomes NaN
+  float up = max3_nan(ref, high, high);
+  if (up == INFINITY) up = NAN;
+  const float f = ref == -INFINITY ? 0.f : ex2(ref - up);
+  ref = up;
+  const uint64_t f2 = pack2(f, f);
+  sum[0] = mul2(sum[0], f2);
+  sum[1] = mul2(sum[1], f2);
+  if (scale_o) {
+#pragma unroll 1
+    for (int c = 0; c < 8; ++c) {
+      uint32_t x[16];
+      tmem_ld16(o_addr + c * 16, x);
+      tmem_wait_ld();
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * f);
+      tmem_st16(o_addr + c * 16, x);
+    }
+  }
+}
+// Half of a tile of P is complete.
+__device__ __forceinline__ void hand_over(uint32_t bar, int lane) {
+  tmem_wait_st();
+  tc_fence_before();
+  __syncwarp();
+  if (lane == 0) mbar_arrive(bar);
 }
 
 __global__ void __launch_bounds__(kThreads, 1)
@@ -69,7 +151,9 @@ attend_tc_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, const 
     }
     if (lane < 2) {
       mbar_init(smem_u32(&sh->s_full[lane]), 1);
-      mbar_init(smem_u32(&sh->p_full[lane]), 4);
+      mbar_init(smem_u32(&sh->p_full[lane][0]), 4);
+      mbar_init(smem_u32(&sh->p_full[lane][1]), 4);
+      mbar_init(smem_u32(&sh->half_done[lane]), 1);
       mbar_init(smem_u32(&sh->o_full[lane]), 1);
       mbar_init(smem_u32(&sh->o_empty[lane]), 4);
     }
@@ -182,10 +266,11 @@ attend_tc_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, const 
         umma_commit(smem_u32(&sh->s_full[i]));
       }
     };
-    auto outputs = [&](int i, uint32_t v_lo, bool accumulate) {
+    auto outputs = [&](int i, int half, uint32_t v_lo, bool accumulate) {
       if (elected) {
 #pragma unroll
-        for (int ks = 0; ks < kTcTile / 16; ++ks) {
+        for (int s4 = 0; s4 < kTcTile / 32; ++s4) {
+          const int ks = half * (kTcTile / 32) + s4;
           const uint32_t b = v_lo + ((1024u >> 4) << 16) + ks * (4096u >> 4);
           umma_tmem_a(tmem + 256 + i * 128, tmem + i * 128 + ks * 8, b | ((uint64_t)r_hi << 32), idesc_o, accumulate || ks > 0);
         }
@@ -215,11 +300,16 @@ attend_tc_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, const 
             ok = wait(&sh->o_empty[i], oe_phase[i], 85);
             oe_phase[i] ^= 1;
           }
-          ok = ok && wait(&sh->p_full[i], p_phase[i], 86);
+          ok = ok && wait(&sh->p_full[i][0], p_phase[i], 86);
+          if (!ok) break;
+          tc_fence_after();
+          outputs(i, 0, r_lo + (uint32_t)v_stage * (kTileBytes >> 4), t > w.t0);
+          if (elected) umma_commit(smem_u32(&sh->half_done[i]));
+          ok = wait(&sh->p_full[i][1], p_phase[i], 79);
           p_phase[i] ^= 1;
           if (!ok) break;
           tc_fence_after();
-          outputs(i, r_lo + (uint32_t)v_stage * (kTileBytes >> 4), t > w.t0);
+          outputs(i, 1, r_lo + (uint32_t)v_stage * (kTileBytes >> 4), true);
           if (i == tiles - 1 && elected) umma_commit(smem_u32(&sh->empty[v_stage]));
           if (more_keys) {
             if (i == 0) {
@@ -245,6 +335,7 @@ attend_tc_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, const 
     const int r = (warp & 3) * 32 + lane;          // row of the tile = lane of tensor memory
     const uint32_t s_addr = tmem + i * 128 + ((uint32_t)((warp & 3) * 32) << 16), o_addr = s_addr + 256;
     const float c2 = fabsf(g.scale) * kLog2e;
+    const uint64_t c22 = pack2(c2, c2);
     const int in_tile = r / g.group;
     uint32_t s_phase = 0, of_phase = 0;
     uint32_t entry = 1;                            // of V of the next tile in the order of the ring
@@ -275,71 +366,87 @@ attend_tc_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, const 
                                       ((e >> 4) & 7) * 128 + (e & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
           fence_proxy_async();
         }
+        if (!dead) tc_fence_after();
         if (!dead && !idle) {
-          tc_fence_after();
-          uint32_t v[4][32];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + c * 32, v[c]);
-          tmem_wait_ld();
-          const bool edge = key0 + kTcTile > least;
-          if (edge) {
-#pragma unroll
-            for (int c = 0; c < 4; ++c)
-#pragma unroll
-              for (int e = 0; e < 32; ++e)
-                if (key0 + c * 32 + e >= lim) v[c][e] = 0xff800000u;
-          }
-          float top[4];
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            top[c] = __uint_as_float(v[c][0]);
-#pragma unroll
-            for (int e = 1; e < 31; e += 2) top[c] = max3_nan(top[c], __uint_as_float(v[c][e]), __uint_as_float(v[c][e + 1]));
-            top[c] = max3_nan(top[c], __uint_as_float(v[c][31]), top[c]);
-          }
-          const float high = max3_nan(max3_nan(top[0], top[1], top[2]), top[3], top[3]) * c2;
-          if (__any_sync(0xffffffffu, real && !(high <= ref + kSlack))) {
-            // a row of infinities or of values that are no numbers has no reference: everything becomes NaN
-            float up = max3_nan(ref, high, high);
-            if (up == INFINITY) up = NAN;
-            const float f = ref == -INFINITY ? 0.f : ex2(ref - up);
-            ref = up;
-            const uint64_t f2 = pack2(f, f);
-            sum[0] = mul2(sum[0], f2);
-            sum[1] = mul2(sum[1], f2);
-            if (t > w.t0) {                        // (the products so far are complete: those of S came behind them)
-#pragma unroll 1
-              for (int c = 0; c < 4; ++c) {
-                uint32_t x[32];
-                tmem_ld32(o_addr + c * 32, x);
-                tmem_wait_ld();
-#pragma unroll
-                for (int e = 0; e < 32; ++e) x[e] = __float_as_uint(__uint_as_float(x[e]) * f);
-                tmem_st32(o_addr + c * 32, x);
+          const uint32_t p_bar = smem_u32(&sh->p_full[i][0]);
+          int from = 0;                            // first chunk of 32 keys that is not handed over yet
+          if (t > w.t0 && key0 + kTcTile <= least) {
+            // With the reference that there is.  P of a half goes over the first columns of S, of which chunk 0 is still in
+            // registers when the half is checked, and goes back if it has to be computed again.
+            uint32_t v0[32], v1[32];
+            float reach = -INFINITY;
+            uint64_t part[2] = {0ull, 0ull};
+            const uint64_t off2 = offset_of(ref);
+            tmem_ld32(s_addr, v0);
+            tmem_wait_ld();
+            tmem_ld32(s_addr + 32, v1);
+            exponentials<true>(v0, c22, off2, s_addr, part, reach);
+            tmem_wait_ld();
+            exponentials<true>(v1, c22, off2, s_addr + 16, part, reach);
+            if (out_of_range(real, part, reach, c2, ref)) {
+              tmem_st32(s_addr, v0);
+              tmem_wait_st();
+            } else {
+              hand_over(p_bar, lane);
+              from = 2;
+              sum[0] = add2(sum[0], part[0]);
+              sum[1] = add2(sum[1], part[1]);
+              part[0] = part[1] = 0ull;
+              reach = -INFINITY;
+              tmem_ld32(s_addr + 64, v0);
+              tmem_wait_ld();
+              tmem_ld32(s_addr + 96, v1);
+              exponentials<true>(v0, c22, off2, s_addr + 32, part, reach);
+              tmem_wait_ld();
+              exponentials<true>(v1, c22, off2, s_addr + 48, part, reach);
+              if (out_of_range(real, part, reach, c2, ref)) {
+                dead = !wait(&sh->half_done[i], s_phase ^ 1, 92);        // the product of the first half with V is under way
+                tc_fence_after();
+              } else {
+                hand_over(p_bar + 8, lane);
+                from = 4;
+                sum[0] = add2(sum[0], part[0]);
+                sum[1] = add2(sum[1], part[1]);
               }
             }
           }
-          const float off = ref == -INFINITY ? 0.f : -ref;
-          const uint64_t c22 = pack2(c2, c2), off2 = pack2(off, off);
+          if (from < 4) {
+            // The maximum first: the first tile of a row, tiles with masked keys, logits far above the reference.
+            const int last = key0 + kTcTile > least ? lim - key0 : kTcTile;
+            float high = -INFINITY;
+            uint32_t v[32];
+#pragma unroll 1
+            for (int c = from; c < 4; ++c) {
+              tmem_ld32(s_addr + c * 32, v);
+              tmem_wait_ld();
+              if (last < kTcTile) {
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint32_t p[16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-              const uint64_t x = fma2(pack2(__uint_as_float(v[c][2 * e]), __uint_as_float(v[c][2 * e + 1])), c22, off2);
-              const uint64_t y = ex2_pair_sfu(x);
-              sum[e & 1] = add2(sum[e & 1], y);
-              float a, b;
-              unpack2(y, a, b);
-              p[e] = pack_bf16(a, b);
+                for (int e = 0; e < 32; ++e)
+                  if (c * 32 + e >= last) v[e] = 0xff800000u;
+              }
+              high = max3_nan(high, max32_nan(v), high);
             }
-            tmem_st16(s_addr + c * 16, p);
+            raise(high * c2, real, ref, sum, t > w.t0 || from > 0, o_addr);
+            const uint64_t off2 = offset_of(ref);
+            float reach = 0.f;
+#pragma unroll 1
+            for (int c = from; c < 4; ++c) {
+              tmem_ld32(s_addr + c * 32, v);
+              tmem_wait_ld();
+              if (last < kTcTile) {
+#pragma unroll
+                for (int e = 0; e < 32; ++e)
+                  if (c * 32 + e >= last) v[e] = 0xff800000u;
+              }
+              exponentials<false>(v, c22, off2, s_addr + c * 16, sum, reach);
+              if (c & 1) hand_over(p_bar + (c >> 1) * 8, lane);
+            }
           }
-          tmem_wait_st();
+        } else {
+          tc_fence_before();
+          __syncwarp();
+          if (lane < 2) mbar_arrive(smem_u32(&sh->p_full[i][lane]));
         }
-        tc_fence_before();
-        __syncwarp();
-        if (lane == 0) mbar_arrive(smem_u32(&sh->p_full[i]));
       }
 
       // the rows' outputs
@@ -348,12 +455,7 @@ attend_tc_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, const 
         of_phase ^= 1;
         tc_fence_after();
       }
-      float total;
-      {
-        float a, b;
-        unpack2(add2(sum[0], sum[1]), a, b);
-        total = a + b;
-      }
+      const float total = total_of(sum);
       const bool whole = w.whole();
       const int h = w.at.h * g.group + r - in_tile * g.group;
       const int64_t row = cs.new_off[w.s] + tok, at = (int64_t)w.slot() * as.rows + i * 128 + r;
