@@ -98,7 +98,7 @@ _SPEC = {"cc_score_window": b"iittttwi", "cc_fuse_prior_pool": b"iittti", "cc_to
          "cc_topk_select_static": b"iitttti", "cc_compact_kv": b"iippttttti",
          "cc_compress_layer": b"iittptttttttwi", "cc_compress_layers": b"iiiLLLtLLLLLLwi",
          "cc_ppl_chunk_scores": b"itiiiiiittti", "cc_select_chunks": b"itiiti",
-         "cc_rope_append": b"iittttttti", "cc_paged_attention": b"iitttttwi", "cc_fork_pages": b"iiiLLiititi"}
+         "cc_rope_append": b"iidbbbnbbbi", "cc_paged_attention": b"iidbbbbfwi", "cc_fork_pages": b"iidiMMhinini"}
 
 
 def load_library(path: Optional[str] = None) -> C.CDLL:
@@ -406,13 +406,6 @@ def _raw_on(ctx: "Context", stream: Optional[int]) -> int:
     return _CURRENT_RAW(ctx.device)
 
 
-def _check_tensors(ctx: "Context", dtype, *tensors) -> None:
-    """Tensors of a call on a cache: of the given type, on the context's device."""
-    for t in tensors:
-        if t is not None and (t.dtype != dtype or t.get_device() != ctx.device):
-            raise ValueError(f"a {dtype} tensor on cuda:{ctx.device} is needed, got {t.dtype} on {t.device}")
-
-
 def _stream(stream: Optional[int]) -> C.c_void_p:
     return C.c_void_p(_raw(stream))
 
@@ -559,28 +552,24 @@ def cc_workspace_views(ctx: Context, desc: Desc, ws: torch.Tensor):
 
 def cc_rope_append(ctx: Context, desc: CacheDesc, q_new, k_new, v_new, positions, q, k, v, stream=None):
     """Rotates the new tokens' queries into ``q`` and appends rotated keys and values to the cache ``k``, ``v``."""
-    _check_tensors(ctx, torch.bfloat16, q_new, k_new, v_new, q, k, v)
-    _check_tensors(ctx, torch.int32, positions)
-    ctx.call("cc_rope_append", desc, q_new, k_new, v_new, positions, q, k, v, _raw_on(ctx, stream))
+    ctx.call("cc_rope_append", desc, ctx.device, q_new, k_new, v_new, positions, q, k, v, _raw_on(ctx, stream))
 
 
 def cc_paged_attention(ctx: Context, desc: CacheDesc, q, k, v, out, lse=None, ws=None, stream=None):
     """Attention of the new tokens over the cache into ``out`` (and ``lse``)."""
-    _check_tensors(ctx, torch.bfloat16, q, k, v, out)
-    _check_tensors(ctx, torch.float32, lse)
     ws = ctx.cache_workspace(desc) if ws is None else ws
-    ctx.call("cc_paged_attention", desc, q, k, v, out, lse, ws, _raw_on(ctx, stream))
+    ctx.call("cc_paged_attention", desc, ctx.device, q, k, v, out, lse, ws, _raw_on(ctx, stream))
 
 
 def cc_fork_pages(ctx: Context, desc: CacheDesc, k_layers, v_layers, parents, child_table, free_pages, stream=None):
     """Child f continues sequence ``parents[f]`` (host integers): its row of ``child_table`` and, in every layer's pools
     ``k_layers`` / ``v_layers``, a copy of the parent's last page in ``free_pages[f]`` where that page is not full."""
-    parents = np.ascontiguousarray(parents, dtype=np.int32)
-    _check_tensors(ctx, torch.bfloat16, *k_layers, *v_layers)
-    _check_tensors(ctx, torch.int32, child_table, free_pages)
-    if len(k_layers) != len(v_layers) or free_pages.numel() < len(parents) or child_table.shape[0] < len(parents):
+    if not isinstance(parents, np.ndarray) or parents.dtype != np.int32:
+        parents = np.ascontiguousarray(parents, dtype=np.int32)
+    children = len(parents)
+    if len(k_layers) != len(v_layers) or free_pages.numel() < children or child_table.shape[0] < children:
         raise ValueError("as many value pools as key pools, a fresh page and a row of child_table per child are needed")
     if not child_table.is_contiguous() or not free_pages.is_contiguous():
         raise ValueError("child_table and free_pages must be contiguous")
-    ctx.call("cc_fork_pages", desc, len(k_layers), k_layers, v_layers, parents.ctypes.data, len(parents), child_table,
+    ctx.call("cc_fork_pages", desc, ctx.device, len(k_layers), k_layers, v_layers, parents, children, child_table,
              child_table.shape[1], free_pages, _raw_on(ctx, stream))

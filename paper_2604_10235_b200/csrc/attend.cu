@@ -12,65 +12,91 @@ namespace cc {
 namespace {
 
 constexpr int kJoinWarps = 8;
+constexpr int kJoinRows = 8;             // blocks per boundary at most
 
-// Joins the parts of the problems that are cut: a block per (boundary between two shares, eight rows), idle unless the
-// boundary is the first inside its problem.  A warp takes a row; the parts follow each other in the order of the CTAs.
+// Joins the parts of the problems that are cut: blocks per (boundary between two shares, rows), idle unless the boundary is the first
+// inside its problem.  A warp takes a row at a time; the parts follow each other in the order of the CTAs.
 //   out = sum_k 2^(m_k - M) o_k / sum_k 2^(m_k - M) l_k
+// Bound by latency (what it reads is in L2): the places of 31 shares in one load, and the first outputs of a row are asked for
+// together with its statistics.
 __global__ void __launch_bounds__(kJoinWarps * 32)
-attend_join_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, const __grid_constant__ AttendSeqs as,
+attend_join_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
                    const AttendWs ws, int grid, const AttendOut o, DeviceStatus* status) {
+  constexpr int kAhead = 8;
   pdl_launch_dependents();
   pdl_wait();
-  const int lane = threadIdx.x & 31, r = blockIdx.y * kJoinWarps + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31;
   const int b = blockIdx.x + 1;                    // the share that begins at the boundary
-  const Place p = ws.place[b], before = ws.place[b - 1];
+  auto place = [&](int share) {
+    const int4 x = share < grid ? __ldcg(reinterpret_cast<const int4*>(ws.place + share)) : make_int4(0, 0, 0, -1);
+    return Place{x.x, x.y, x.z, x.w};
+  };
+  const Place near = place(b - 1 + lane);          // of shares b - 1, b, ...
+  const Place p = {__shfl_sync(0xffffffffu, near.h, 1), __shfl_sync(0xffffffffu, near.i, 1), __shfl_sync(0xffffffffu, near.b, 1),
+                   __shfl_sync(0xffffffffu, near.tile, 1)};
   auto inside = [&](const Place& x) { return x.tile > 0 && x.h == p.h && x.i == p.i && x.b == p.b; };
-  if (p.tile <= 0 || inside(before)) return;
-  const int s = as.src[p.i], T = cs.new_off[s + 1] - cs.new_off[s];
-  const int in_tile = (r & 127) / g.group, t = p.b * as.block_tokens + (r >> 7) * as.tile_tokens + in_tile;
-  if (in_tile >= as.tile_tokens || t >= T) return;
-  int last = b;                                    // the last share with a part of the problem
-  while (last + 1 < grid && inside(ws.place[last + 1])) ++last;
-  const int parts = last - b + 2;
-  // part 0 is the end of share b - 1, part k the beginning of share b - 1 + k
-  auto entry = [&](int k) { return (int64_t)(k == 0 ? 2 * (b - 1) + 1 : 2 * (b - 1 + k)) * as.rows + r; };
-  float top = -INFINITY;
-  for (int k = lane; k < parts; k += 32) top = fmaxf(top, ws.stat[entry(k)].x);
-#pragma unroll
-  for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-  float total = 0.f;
-  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int k0 = 0; k0 < parts; k0 += 32) {
-    float f = 0.f;
-    if (k0 + lane < parts) {
-      const float2 st = ws.stat[entry(k0 + lane)];
-      f = st.x == -INFINITY ? 0.f : ex2(st.x - top);
-      total += f * st.y;
-    }
-    const int m = min(32, parts - k0);
-#pragma unroll 4
-    for (int k = 0; k < m; ++k) {
-      const float w = __shfl_sync(0xffffffffu, f, k);
-      const float4 x = __ldcg(reinterpret_cast<const float4*>(ws.out + entry(k0 + k) * kHeadDim) + lane);
-      v.x = fmaf(w, x.x, v.x);
-      v.y = fmaf(w, x.y, v.y);
-      v.z = fmaf(w, x.z, v.z);
-      v.w = fmaf(w, x.w, v.w);
+  unsigned in = __ballot_sync(0xffffffffu, inside(near));
+  if (p.tile <= 0 || (in & 1u)) return;
+  if (p.h >= g.hkv || p.i >= as.num || p.b >= as.seq[p.i].blocks) return;      // (another call wrote to this workspace)
+  int parts = __ffs(~(in >> 1));                   // shares b, b + 1, ... that begin inside, and the one before
+  if (in == 0xfffffffeu) {
+    for (int s0 = b + 31;; s0 += 32) {
+      in = __ballot_sync(0xffffffffu, inside(place(s0 + lane)));
+      parts += in == 0xffffffffu ? 32 : __ffs(~in) - 1;
+      if (in != 0xffffffffu) break;
     }
   }
+  const int T = as.seq[p.i].T, n = attend_len(as, g, p.i, status);
+  for (int r = blockIdx.y * kJoinWarps + (threadIdx.x >> 5); r < as.rows; r += gridDim.y * kJoinWarps) {
+    const int in_tile = (r & 127) / g.group, t = p.b * as.block_tokens + (r >> 7) * as.tile_tokens + in_tile;
+    if (in_tile >= as.tile_tokens || t >= T) continue;
+    // part 0 is the end of share b - 1, part k the beginning of share b - 1 + k
+    auto entry = [&](int k) { return (int64_t)(k == 0 ? 2 * (b - 1) + 1 : 2 * (b - 1 + k)) * as.rows + r; };
+    auto output = [&](int k) { return __ldcg(reinterpret_cast<const float4*>(ws.out + entry(k) * kHeadDim) + lane); };
+    float4 x[kAhead];
 #pragma unroll
-  for (int d = 16; d > 0; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
-  const int n = cache_len(cs, g, s, status);
-  const bool none = (g.causal ? n - T + t + 1 : n) <= 0;
-  const float inv = none ? 0.f : 1.0f / total;
-  const int64_t tok = cs.new_off[s] + t;
-  const int h = p.h * g.group + (r & 127) - in_tile * g.group;
-  const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x * inv, v.y * inv), hi = __floats2bfloat162_rn(v.z * inv, v.w * inv);
-  uint2 bits;
-  bits.x = *reinterpret_cast<const uint32_t*>(&lo);
-  bits.y = *reinterpret_cast<const uint32_t*>(&hi);
-  *reinterpret_cast<uint2*>(o.out + tok * g.out_tok + h * g.out_head + lane * 4) = bits;
-  if (o.lse && lane == 0) o.lse[tok * g.hq + h] = none ? -INFINITY : (top + log2f(total)) * 0.6931471805599453f;
+    for (int k = 0; k < kAhead; ++k) x[k] = k < parts ? output(k) : make_float4(0.f, 0.f, 0.f, 0.f);
+    const float2 first = lane < parts ? __ldcg(ws.stat + entry(lane)) : make_float2(-INFINITY, 0.f);
+    float top = first.x;
+    for (int k = 32 + lane; k < parts; k += 32) top = fmaxf(top, __ldcg(ws.stat + entry(k)).x);
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+    float total = 0.f;
+    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+    auto add = [&](float w, const float4& y) {
+      v.x = fmaf(w, y.x, v.x);
+      v.y = fmaf(w, y.y, v.y);
+      v.z = fmaf(w, y.z, v.z);
+      v.w = fmaf(w, y.w, v.w);
+    };
+    for (int k0 = 0; k0 < parts; k0 += 32) {
+      const float2 st = k0 == 0 ? first : k0 + lane < parts ? __ldcg(ws.stat + entry(k0 + lane)) : make_float2(-INFINITY, 0.f);
+      const float f = st.x == -INFINITY ? 0.f : ex2(st.x - top);
+      total += f * st.y;
+      const int m = min(32, parts - k0);
+      if (k0 == 0) {
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+          const float w = __shfl_sync(0xffffffffu, f, k);
+          if (k < m) add(w, x[k]);
+        }
+      }
+#pragma unroll 8
+      for (int k = k0 == 0 ? kAhead : 0; k < m; ++k) add(__shfl_sync(0xffffffffu, f, k), output(k0 + k));
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
+    const bool none = (g.causal ? n - T + t + 1 : n) <= 0;
+    const float inv = none ? 0.f : 1.0f / total;
+    const int64_t tok = as.seq[p.i].row0 + t;
+    const int h = p.h * g.group + (r & 127) - in_tile * g.group;
+    const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x * inv, v.y * inv), hi = __floats2bfloat162_rn(v.z * inv, v.w * inv);
+    uint2 bits;
+    bits.x = *reinterpret_cast<const uint32_t*>(&lo);
+    bits.y = *reinterpret_cast<const uint32_t*>(&hi);
+    *reinterpret_cast<uint2*>(o.out + tok * g.out_tok + h * g.out_head + lane * 4) = bits;
+    if (o.lse && lane == 0) o.lse[tok * g.hq + h] = none ? -INFINITY : (top + log2f(total)) * 0.6931471805599453f;
+  }
 }
 
 // The launches of a call: sequences with at most 16 query rows per KV head go to the kernel for few rows, the others to the
@@ -79,35 +105,52 @@ struct AttendPlan {
   AttendSeqs as;
   int grid;
 };
-struct AttendPlans { AttendPlan rows, tc; };
+constexpr int64_t kFewKeys = 400000;      // (keys x KV heads)
+struct AttendPlans {
+  AttendPlan rows, tc;
+  bool too_much;                                   // 2^31 tiles and more
+};
 
 AttendPlans plan_attend(const CacheSeqs& cs, const CacheGeom& g, int sm_count) {
   AttendPlans p = {};
   AttendSeqs& few = p.rows.as;
-  few.tile_keys = kRowsTile;
+  few.tile_shift = 6;
+  static_assert(kRowsTile == 1 << 6 && kTcTile == 1 << 7, "tiles");
   few.rows = kRowsMost;
   few.block_tokens = few.tile_tokens = std::max(1, kRowsMost / g.group);
   few.start_weight = 1;
   AttendSeqs& many = p.tc.as;
-  many.tile_keys = kTcTile;
+  many.tile_shift = 7;
   many.rows = 2 * kTcTile;
   many.tile_tokens = kTcTile / g.group;
   many.block_tokens = 2 * many.tile_tokens;
-  many.start_weight = 2;
+  many.start_weight = 3;              // (2: ragged chunks 273 -> 254 us with 3; 4: 257)
+  // A batch of both kinds goes to the tensor-core kernel as a whole unless the sequences with few rows have many keys: that kernel
+  // takes a quarter longer over them (64 tokens over 245000 keys x 8 heads: 213 against 168 us) and a launch of their own costs
+  // 10 us (16 sequences of 1 to 8 tokens, four of them with few rows: 58.6 against 48.7 us).
+  int64_t few_keys = 0;
+  bool mixed = false;
+  auto is_few = [&](int T) { return (int64_t)T * g.group <= kRowsMost; };
+  for (int s = 0; s < cs.num_seqs; ++s) {
+    const int T = cs.new_off[s + 1] - cs.new_off[s];
+    if (is_few(T)) few_keys += T > 0 ? cs.kv_len[s] : 0;
+    else mixed = true;
+  }
+  const bool apart = !mixed || few_keys * g.hkv > kFewKeys;
   for (int s = 0; s < cs.num_seqs; ++s) {
     const int T = cs.new_off[s + 1] - cs.new_off[s];
     if (T == 0) continue;
-    AttendSeqs& as = (int64_t)T * g.group <= kRowsMost ? few : many;
+    AttendSeqs& as = is_few(T) && apart ? few : many;
+    as.seq[as.num] = AttendSeq{cs.new_off[s], T, cs.kv_len[s], (T + as.block_tokens - 1) / as.block_tokens};
     as.src[as.num++] = (uint8_t)s;
   }
   for (AttendPlan* x : {&p.rows, &p.tc}) {
     const AttendSeqs& as = x->as;
     int64_t total = 0;                             // of the weights (attend_weigh), at the longest
-    for (int i = 0; i < as.num; ++i) {
-      const int s = as.src[i];
-      const int64_t blocks = (cs.new_off[s + 1] - cs.new_off[s] + as.block_tokens - 1) / as.block_tokens;
-      total += blocks * (as.start_weight + (cs.kv_len[s] + as.tile_keys - 1) / as.tile_keys) * g.hkv;
-    }
+    for (int i = 0; i < as.num; ++i)
+      total += (int64_t)as.seq[i].blocks * (as.start_weight + ((as.seq[i].n + (1 << as.tile_shift) - 1) >> as.tile_shift));
+    total *= g.hkv;
+    if (total >> 31) p.too_much = true;
     x->grid = (int)std::min<int64_t>(total, sm_count);
   }
   return p;
@@ -139,16 +182,18 @@ CUresult encode_queries(EncodeTiledFn encode, const CacheSeqs& cs, const CacheGe
 
 }  // namespace
 
-cudaError_t launch_attend_join(const Launch& L, const CacheSeqs& cs, const CacheGeom& g, const AttendSeqs& as, const AttendWs& ws,
+cudaError_t launch_attend_join(const Launch& L, const CacheGeom& g, const AttendSeqs& as, const AttendWs& ws,
                                int grid, const AttendOut& o) {
   if (grid < 2) return cudaSuccess;
-  return launch_pdl(attend_join_kernel, dim3((unsigned)(grid - 1), (unsigned)((as.rows + kJoinWarps - 1) / kJoinWarps)),
-                    dim3(kJoinWarps * 32), 0, L.stream, 1, cs, g, as, ws, grid, o, L.status);
+  const int y = std::min((as.rows + kJoinWarps - 1) / kJoinWarps, kJoinRows);
+  return launch_pdl(attend_join_kernel, dim3((unsigned)(grid - 1), (unsigned)y),
+                    dim3(kJoinWarps * 32), 0, L.stream, 1, g, as, ws, grid, o, L.status);
 }
 
 size_t attend_ws_bytes(const CacheSeqs& cs, const CacheGeom& g, int sm_count) {
   const AttendPlans p = plan_attend(cs, g, sm_count);          // one launch after the other uses it
-  return std::max(attend_ws_size(p.rows.grid, p.rows.as.rows), attend_ws_size(p.tc.grid, p.tc.as.rows));
+  if (p.too_much) return 0;
+  return std::max<size_t>({256, attend_ws_size(p.rows.grid, p.rows.as.rows), attend_ws_size(p.tc.grid, p.tc.as.rows)});
 }
 
 cudaError_t launch_attend(const Launch& L, const CacheSeqs& cs, const CacheGeom& g, const void* q, const void* k, const void* v,
@@ -157,6 +202,7 @@ cudaError_t launch_attend(const Launch& L, const CacheSeqs& cs, const CacheGeom&
   const EncodeTiledFn encode = (EncodeTiledFn)encode_fn;
   const AttendOut o = {(uint16_t*)out, lse};
   const AttendPlans p = plan_attend(cs, g, L.sm_count);
+  if (p.too_much) return cudaErrorInvalidConfiguration;
   CUtensorMap q_map, k_map, v_map;
   auto pools = [&](int tile_keys) {
     CUresult r = encode_pool(encode, g, k, tile_keys, &k_map);
@@ -166,18 +212,18 @@ cudaError_t launch_attend(const Launch& L, const CacheSeqs& cs, const CacheGeom&
   };
   cudaError_t e = cudaSuccess;
   if (p.tc.as.num > 0) {
-    if (!pools(p.tc.as.tile_keys)) return cudaErrorUnknown;
+    if (!pools(1 << p.tc.as.tile_shift)) return cudaErrorUnknown;
     *drv_err = (int)encode_queries(encode, cs, g, q, p.tc.as.tile_tokens, &q_map);
     if (*drv_err != 0) return cudaErrorUnknown;
     const AttendWs w = attend_ws(ws, p.tc.grid, p.tc.as.rows);
-    e = launch_attend_tc(L, cs, g, p.tc.as, w, p.tc.grid, o, q_map, k_map, v_map);
-    if (e == cudaSuccess) e = launch_attend_join(L, cs, g, p.tc.as, w, p.tc.grid, o);
+    e = launch_attend_tc(L, g, p.tc.as, w, p.tc.grid, o, q_map, k_map, v_map);
+    if (e == cudaSuccess) e = launch_attend_join(L, g, p.tc.as, w, p.tc.grid, o);
   }
   if (e == cudaSuccess && p.rows.as.num > 0) {
-    if (!pools(p.rows.as.tile_keys)) return cudaErrorUnknown;
+    if (!pools(1 << p.rows.as.tile_shift)) return cudaErrorUnknown;
     const AttendWs w = attend_ws(ws, p.rows.grid, p.rows.as.rows);
-    e = launch_attend_rows(L, cs, g, p.rows.as, w, p.rows.grid, o, q, k_map, v_map);
-    if (e == cudaSuccess) e = launch_attend_join(L, cs, g, p.rows.as, w, p.rows.grid, o);
+    e = launch_attend_rows(L, g, p.rows.as, w, p.rows.grid, o, q, k_map, v_map);
+    if (e == cudaSuccess) e = launch_attend_join(L, g, p.rows.as, w, p.rows.grid, o);
   }
   return e;
 }

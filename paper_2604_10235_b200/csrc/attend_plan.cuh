@@ -14,72 +14,79 @@
 
 namespace cc {
 
+// One sequence of a launch: first row of its new tokens, their number, n_s or its upper bound, blocks of new tokens.
+struct __align__(16) AttendSeq { int row0, T, n, blocks; };
+
 struct AttendSeqs {            // the sequences of one launch
   int num;                     // sequences with new tokens that this kernel takes
   int block_tokens;            // new tokens per block
   int tile_tokens;             // of them in each 128 rows: row r of a block is row r % 128 of its tile r / 128, token
                                // (r % 128) / group of the tile
-  int tile_keys;               // keys per tile
+  int tile_shift;              // keys per tile = 1 << tile_shift
   int start_weight;            // weight of a problem's start, in tiles (at least 1)
   int rows;                    // rows of a block (and of a partial result)
+  AttendSeq seq[CC_MAX_SEQS];
   uint8_t src[CC_MAX_SEQS];    // index of the sequence in the call
 };
 
 // A place in the list of problems: `tile` is the first tile of the problem behind the place.
-struct Place { int h, i, b, tile; };         // head, entry of AttendSeqs, block
+struct __align__(16) Place { int h, i, b, tile; };         // head, entry of AttendSeqs, block
 
 struct AttendShare {           // shared memory
-  long long weight[CC_MAX_SEQS + 1];         // of the sequences before, of one head
-  int len[CC_MAX_SEQS];                      // n_s by entry
+  AttendSeq seq[CC_MAX_SEQS];                // n as the call finds it
+  unsigned weight[CC_MAX_SEQS + 1];          // of the sequences before, of one head (all heads together: below 2^31)
   Place from, to;
 };
 
-__device__ __forceinline__ int attend_limit(const CacheSeqs& cs, const CacheGeom& g, const AttendSeqs& as, int s, int n, int b) {
-  if (!g.causal) return n;
-  const int T = cs.new_off[s + 1] - cs.new_off[s];
-  const int last = min(T, (b + 1) * as.block_tokens);
-  return max(0, n - T + last);
+// n_s as the call finds it.
+__device__ __forceinline__ int attend_len(const AttendSeqs& as, const CacheGeom& g, int i, DeviceStatus* st) {
+  const int most = as.seq[i].n;
+  if (g.dev_lens == nullptr) return most;
+  const int n = g.dev_lens[as.src[i]];
+  if (n >= 0 && n <= most) return n;
+  report_error(st, CC_ERR_DEVICE_FLAG, 600);
+  return n < 0 ? 0 : most;
+}
+// Keys that the block's last token attends to.
+__device__ __forceinline__ int attend_limit(const AttendSeq& q, int block_tokens, int causal, int b) {
+  return causal ? max(0, q.n - q.T + min(q.T, (b + 1) * block_tokens)) : q.n;
 }
 // Tiles of a block: those that hold a key which one of its tokens attends to.
-__device__ __forceinline__ int attend_tiles(const CacheSeqs& cs, const CacheGeom& g, const AttendSeqs& as, int s, int n, int b) {
-  return (attend_limit(cs, g, as, s, n, b) + as.tile_keys - 1) / as.tile_keys;
-}
-__device__ __forceinline__ int attend_blocks(const CacheSeqs& cs, const AttendSeqs& as, int s) {
-  return (cs.new_off[s + 1] - cs.new_off[s] + as.block_tokens - 1) / as.block_tokens;
+__device__ __forceinline__ int attend_tiles(const AttendSeq& q, const AttendSeqs& as, int causal, int b) {
+  return (attend_limit(q, as.block_tokens, causal, b) + (1 << as.tile_shift) - 1) >> as.tile_shift;
 }
 
-// Fills sh->len and sh->weight; all threads of the block, which must synchronise afterwards (twice inside).
-__device__ __forceinline__ void attend_weigh(const CacheSeqs& cs, const CacheGeom& g, const AttendSeqs& as, AttendShare* sh,
-                                             DeviceStatus* st) {
+// Fills sh->seq and sh->weight; all threads of the block, which must synchronise afterwards.
+__device__ __forceinline__ void attend_weigh(const CacheGeom& g, const AttendSeqs& as, AttendShare* sh, DeviceStatus* st) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+  bool blocks = false;
   for (int i = threadIdx.x; i < as.num; i += blockDim.x) {
-    const int s = as.src[i], n = cache_len(cs, g, s, st);
-    sh->len[i] = n;
-    const int nb = attend_blocks(cs, as, s);
-    if (nb == 1) sh->weight[i + 1] = as.start_weight + attend_tiles(cs, g, as, s, n, 0);
-    else if (!g.causal) sh->weight[i + 1] = (long long)nb * (as.start_weight + attend_tiles(cs, g, as, s, n, 0));
+    AttendSeq q = as.seq[i];
+    q.n = attend_len(as, g, i, st);
+    sh->seq[i] = q;
+    // (of a causal chunk of several blocks each block has a limit of its own: below)
+    if (q.blocks == 1 || !g.causal) sh->weight[i + 1] = (unsigned)q.blocks * (as.start_weight + attend_tiles(q, as, g.causal, 0));
+    else blocks = true;
   }
-  __syncthreads();
-  if (g.causal) {
+  if (__syncthreads_or(blocks)) {
     for (int i = warp; i < as.num; i += warps) {
-      const int s = as.src[i], n = sh->len[i], nb = attend_blocks(cs, as, s);
-      if (nb == 1) continue;
-      long long sum = 0;
-      for (int b = lane; b < nb; b += 32) sum += as.start_weight + attend_tiles(cs, g, as, s, n, b);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+      const AttendSeq q = sh->seq[i];
+      if (q.blocks == 1) continue;
+      unsigned sum = 0;
+      for (int b = lane; b < q.blocks; b += 32) sum += as.start_weight + attend_tiles(q, as, g.causal, b);
+      sum = __reduce_add_sync(0xffffffffu, sum);
       if (lane == 0) sh->weight[i + 1] = sum;
     }
     __syncthreads();
   }
   if (warp == 0) {                                 // running sums: two entries per lane
     static_assert(CC_MAX_SEQS == 64, "two entries per lane");
-    const long long a = 2 * lane < as.num ? sh->weight[2 * lane + 1] : 0;
-    const long long b = 2 * lane + 1 < as.num ? sh->weight[2 * lane + 2] : 0;
-    long long run = a + b;
+    const unsigned a = 2 * lane < as.num ? sh->weight[2 * lane + 1] : 0;
+    const unsigned b = 2 * lane + 1 < as.num ? sh->weight[2 * lane + 2] : 0;
+    unsigned run = a + b;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const long long up = __shfl_up_sync(0xffffffffu, run, o);
+      const unsigned up = __shfl_up_sync(0xffffffffu, run, o);
       if (lane >= o) run += up;
     }
     if (lane == 0) sh->weight[0] = 0;
@@ -90,43 +97,45 @@ __device__ __forceinline__ void attend_weigh(const CacheSeqs& cs, const CacheGeo
 
 // CTAs that get a share.
 __device__ __forceinline__ int attend_workers(const AttendSeqs& as, const AttendShare* sh, int hkv, int grid) {
-  const long long total = sh->weight[as.num] * hkv;
-  return total < grid ? (int)total : grid;
+  return (int)min(sh->weight[as.num] * (unsigned)hkv, (unsigned)grid);
 }
 
 // The place at which the share of CTA `cta` of `workers` begins (cta == workers: behind everything); one whole warp.
-__device__ __forceinline__ Place attend_place(const CacheSeqs& cs, const CacheGeom& g, const AttendSeqs& as,
-                                              const AttendShare* sh, int cta, int workers) {
+__device__ __forceinline__ Place attend_place(const CacheGeom& g, const AttendSeqs& as, const AttendShare* sh, int cta, int workers) {
   const int lane = threadIdx.x & 31;
-  const long long per_head = sh->weight[as.num], total = per_head * g.hkv;
+  const unsigned per_head = sh->weight[as.num], total = per_head * (unsigned)g.hkv;
   Place p = {g.hkv, 0, 0, 0};
   if (cta >= workers) return p;
-  // total * cta fits: 2^31 tokens / 64 keys x 2^31 / 128 heads stay far below 2^53
-  const long long at = total / workers * cta + total % workers * cta / workers;
+  const unsigned each = total / (unsigned)workers, extra = total - each * (unsigned)workers;
+  const unsigned at = each * (unsigned)cta + extra * (unsigned)cta / (unsigned)workers;          // floor(total * cta / workers)
   p.h = (int)(at / per_head);
-  long long rest = at - per_head * p.h;
+  unsigned rest = at - per_head * (unsigned)p.h;
   const int e0 = 2 * lane, e1 = 2 * lane + 1;
   const bool in0 = e0 < as.num && sh->weight[e0] <= rest && rest < sh->weight[e0 + 1];
   const bool in1 = e1 < as.num && sh->weight[e1] <= rest && rest < sh->weight[e1 + 1];
   const unsigned m0 = __ballot_sync(0xffffffffu, in0), m1 = __ballot_sync(0xffffffffu, in1);
   p.i = m0 ? 2 * (__ffs(m0) - 1) : 2 * (__ffs(m1) - 1) + 1;
   rest -= sh->weight[p.i];
-  const int s = as.src[p.i], n = sh->len[p.i], nb = attend_blocks(cs, as, s);
-  for (int b0 = 0; b0 < nb; b0 += 32) {
+  const AttendSeq q = sh->seq[p.i];
+  if (q.blocks == 1) {
+    p.tile = max(0, (int)rest - as.start_weight);
+    return p;
+  }
+  for (int b0 = 0; b0 < q.blocks; b0 += 32) {
     const int b = b0 + lane;
-    const long long w = b < nb ? as.start_weight + attend_tiles(cs, g, as, s, n, b) : 0;
-    long long run = w;
+    const unsigned w = b < q.blocks ? as.start_weight + attend_tiles(q, as, g.causal, b) : 0;
+    unsigned run = w;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const long long up = __shfl_up_sync(0xffffffffu, run, o);
+      const unsigned up = __shfl_up_sync(0xffffffffu, run, o);
       if (lane >= o) run += up;
     }
-    const unsigned m = __ballot_sync(0xffffffffu, b < nb && rest < run);
+    const unsigned m = __ballot_sync(0xffffffffu, b < q.blocks && rest < run);
     if (m) {
       const int l = __ffs(m) - 1;
-      const long long before = __shfl_sync(0xffffffffu, run - w, l);
+      const unsigned before = __shfl_sync(0xffffffffu, run - w, l);
       p.b = b0 + l;
-      p.tile = (int)max(0LL, rest - before - as.start_weight);
+      p.tile = max(0, (int)(rest - before) - as.start_weight);
       break;
     }
     rest -= __shfl_sync(0xffffffffu, run, 31);
@@ -134,47 +143,59 @@ __device__ __forceinline__ Place attend_place(const CacheSeqs& cs, const CacheGe
   return p;
 }
 
+// The whole beginning of a kernel: sh->from and sh->to, and the workspace's entry.  Where the lengths are the call's own, all of it
+// is arithmetic on the parameters and runs before the launch before this one has ended.
+__device__ __forceinline__ void attend_share(const CacheGeom& g, const AttendSeqs& as, AttendShare* sh, Place* places,
+                                             DeviceStatus* st) {
+  const int warp = threadIdx.x >> 5;
+  if (g.dev_lens) pdl_wait();
+  attend_weigh(g, as, sh, st);
+  __syncthreads();
+  const int workers = attend_workers(as, sh, g.hkv, gridDim.x);
+  Place p = {0, 0, 0, -1};
+  if (warp < 2) {
+    p = attend_place(g, as, sh, blockIdx.x + warp, workers);
+    if ((threadIdx.x & 31) == 0) (warp == 0 ? sh->from : sh->to) = p;
+  }
+  pdl_wait();
+  if (threadIdx.x == 0) places[blockIdx.x] = (int)blockIdx.x < workers ? p : Place{0, 0, 0, -1};
+  __syncthreads();
+}
+
 // The problems of a share one after the other.
 struct AttendWalk {
   Place at, to;
-  int s, n, T, n_blocks, tiles;      // of the current problem
+  AttendSeq q;                       // of the current problem
+  int limit, tiles;                  // keys that any of its tokens attends to, tiles that hold them
   int t0, t1;                        // tiles of it in this share
   __device__ __forceinline__ bool same(const Place& a, const Place& b) const { return a.h == b.h && a.i == b.i && a.b == b.b; }
-  __device__ __forceinline__ void seq(const CacheSeqs& cs, const AttendSeqs& as, const AttendShare* sh) {
-    s = as.src[at.i];
-    n = sh->len[at.i];
-    T = cs.new_off[s + 1] - cs.new_off[s];
-    n_blocks = attend_blocks(cs, as, s);
-  }
-  __device__ __forceinline__ bool open(const CacheSeqs& cs, const CacheGeom& g, const AttendSeqs& as) {
+  __device__ __forceinline__ bool open(const CacheGeom& g, const AttendSeqs& as, const AttendShare* sh) {
     if (at.h >= g.hkv) return false;
     const bool last = same(at, to);
     if (last && to.tile == 0) return false;        // the problem belongs to the next share
-    tiles = attend_tiles(cs, g, as, s, n, at.b);
+    q = sh->seq[at.i];
+    limit = attend_limit(q, as.block_tokens, g.causal, at.b);
+    tiles = (limit + (1 << as.tile_shift) - 1) >> as.tile_shift;
     t0 = at.tile;
     t1 = last ? to.tile : tiles;
     return t0 < t1 || tiles == 0;
   }
-  __device__ __forceinline__ bool first(const CacheSeqs& cs, const CacheGeom& g, const AttendSeqs& as, const AttendShare* sh) {
+  __device__ __forceinline__ bool first(const CacheGeom& g, const AttendSeqs& as, const AttendShare* sh) {
     at = sh->from;
     to = sh->to;
-    if (at.h >= g.hkv) return false;
-    seq(cs, as, sh);
-    return open(cs, g, as);
+    return open(g, as, sh);
   }
-  __device__ __forceinline__ bool next(const CacheSeqs& cs, const CacheGeom& g, const AttendSeqs& as, const AttendShare* sh) {
+  __device__ __forceinline__ bool next(const CacheGeom& g, const AttendSeqs& as, const AttendShare* sh) {
     if (same(at, to)) return false;
     at.tile = 0;
-    if (++at.b == n_blocks) {
+    if (++at.b == q.blocks) {
       at.b = 0;
       if (++at.i == as.num) {
         at.i = 0;
         ++at.h;
       }
-      if (at.h >= g.hkv) return false;
-      seq(cs, as, sh);
     }
-    return open(cs, g, as);
+    return open(g, as, sh);
   }
   __device__ __forceinline__ bool whole() const { return t0 == 0 && t1 == tiles; }
   // The entry of the workspace for what this share has of a cut problem: a share begins inside one problem at most and
@@ -206,12 +227,12 @@ struct AttendOut {
 };
 
 // Launches the join of cut problems (attend.cu).
-cudaError_t launch_attend_join(const Launch& L, const CacheSeqs& cs, const CacheGeom& g, const AttendSeqs& as, const AttendWs& ws,
+cudaError_t launch_attend_join(const Launch& L, const CacheGeom& g, const AttendSeqs& as, const AttendWs& ws,
                                int grid, const AttendOut& o);
 // The kernel for up to 16 rows per block (attend_rows.cu) and the one for blocks of 256 (attend_tc.cu).
-cudaError_t launch_attend_rows(const Launch& L, const CacheSeqs& cs, const CacheGeom& g, const AttendSeqs& as, const AttendWs& ws,
+cudaError_t launch_attend_rows(const Launch& L, const CacheGeom& g, const AttendSeqs& as, const AttendWs& ws,
                                int grid, const AttendOut& o, const void* q, const CUtensorMap& k_map, const CUtensorMap& v_map);
-cudaError_t launch_attend_tc(const Launch& L, const CacheSeqs& cs, const CacheGeom& g, const AttendSeqs& as, const AttendWs& ws,
+cudaError_t launch_attend_tc(const Launch& L, const CacheGeom& g, const AttendSeqs& as, const AttendWs& ws,
                              int grid, const AttendOut& o, const CUtensorMap& q_map, const CUtensorMap& k_map,
                              const CUtensorMap& v_map);
 constexpr int kTcTile = 128;         // keys per tile of attend_tc.cu, and query rows per tile (two tiles a block)

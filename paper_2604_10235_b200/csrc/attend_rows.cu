@@ -71,7 +71,7 @@ __device__ __forceinline__ uint32_t tile_at(int key, int c) {
 }
 
 __global__ void __launch_bounds__(kThreads, 1)
-attend_rows_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, const __grid_constant__ AttendSeqs as,
+attend_rows_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
                    const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map,
                    const uint16_t* __restrict__ q, const AttendOut o, const AttendWs ws, DeviceStatus* status) {
   extern __shared__ uint8_t dyn[];
@@ -79,6 +79,10 @@ attend_rows_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, cons
   Shared* sh = reinterpret_cast<Shared*>(ring + (size_t)kStages * 2 * kTileBytes);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_launch_dependents();
+  if (warp == 1 && elect_one()) {
+    prefetch_map(&k_map);
+    prefetch_map(&v_map);
+  }
   if (warp == 0) {
     if (lane < kStages) {
       mbar_init(smem_u32(&sh->full[lane]), 1);
@@ -94,22 +98,7 @@ attend_rows_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, cons
   for (int i = threadIdx.x; i < 2 * kRowsMost * kQPitch / 16; i += kThreads)     // rows that no problem has stay zero
     reinterpret_cast<uint4*>(sh->q)[i] = make_uint4(0u, 0u, 0u, 0u);
   fence_proxy_async();
-  pdl_wait();
-  attend_weigh(cs, g, as, &sh->share, status);
-  __syncthreads();
-  const int workers = attend_workers(as, &sh->share, g.hkv, gridDim.x);
-  if (warp < 2) {
-    const Place p = attend_place(cs, g, as, &sh->share, blockIdx.x + warp, workers);
-    if (lane == 0) {
-      if (warp == 0) {
-        sh->share.from = p;
-        ws.place[blockIdx.x] = blockIdx.x < workers ? p : Place{0, 0, 0, -1};
-      } else {
-        sh->share.to = p;
-      }
-    }
-  }
-  __syncthreads();
+  attend_share(g, as, &sh->share, ws.place, status);
   const BoundedWait pipe = {&sh->abort_flag, &status->code};
 
   if (warp == 0) {
@@ -125,20 +114,20 @@ attend_rows_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, cons
     int stage = 0, seg = 0;
     uint32_t phase = 0;
     bool ok = true;
-    for (bool more = w.first(cs, g, as, &sh->share); more && ok; more = w.next(cs, g, as, &sh->share), ++seg) {
+    for (bool more = w.first(g, as, &sh->share); more && ok; more = w.next(g, as, &sh->share), ++seg) {
       const int buf = seg & 1;
       if (!bounded_wait(pipe, &sh->q_empty[buf], ((seg >> 1) & 1) ^ 1, CC_ERR_TIMEOUT, 70)) break;
-      const int rows = min(as.block_tokens, w.T - w.at.b * as.block_tokens) * g.group;
+      const int rows = min(as.block_tokens, w.q.T - w.at.b * as.block_tokens) * g.group;
       const uint32_t qb = smem_u32(&sh->q_full[buf]);
       if (elected) mbar_expect_tx(qb, (uint32_t)rows * kHeadDim * 2);
       __syncwarp();
       if (lane < rows) {
         const int t = lane / g.group, h = w.at.h * g.group + lane - t * g.group;
-        const int64_t tok = cs.new_off[w.s] + w.at.b * as.block_tokens + t;
+        const int64_t tok = w.q.row0 + w.at.b * as.block_tokens + t;
         bulk_load(smem_u32(sh->q[buf]) + lane * kQPitch, q + tok * g.q_tok + h * g.q_head, kHeadDim * 2, qb);
       }
-      const int limit = attend_limit(cs, g, as, w.s, w.n, w.at.b);
-      const int32_t* table = g.table + (int64_t)w.s * g.table_stride;
+      const int limit = w.limit;
+      const int32_t* table = g.table + (int64_t)as.src[w.at.i] * g.table_stride;
       for (int t = w.t0; t < w.t1; ++t) {
         const int key = t * kRowsTile + lane * span;           // first key of this lane's copy
         const bool mine = lane < copies && key < limit;
@@ -175,7 +164,7 @@ attend_rows_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, cons
     AttendWalk w;
     int it = 0, seg = 0;             // tiles and problems of the share so far
     bool dead = false;
-    for (bool more = w.first(cs, g, as, &sh->share); more; more = w.next(cs, g, as, &sh->share), ++seg) {
+    for (bool more = w.first(g, as, &sh->share); more; more = w.next(g, as, &sh->share), ++seg) {
       const int buf = seg & 1;
       if (!dead) dead = !bounded_wait(pipe, &sh->q_full[buf], (seg >> 1) & 1, CC_ERR_TIMEOUT, 72);
       uint32_t qa[8][4];
@@ -187,15 +176,15 @@ attend_rows_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, cons
         if (lane == 0) mbar_arrive(smem_u32(&sh->q_empty[buf]));
       }
       const int tok0 = w.at.b * as.block_tokens;
-      const int real = min(as.block_tokens, w.T - tok0) * g.group;       // rows of the problem
+      const int real = min(as.block_tokens, w.q.T - tok0) * g.group;       // rows of the problem
       int lim[2];                                                        // keys that rows r0 and r0 + 8 attend to
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int r = r0 + 8 * i;
-        lim[i] = r < real ? (g.causal ? max(0, w.n - w.T + tok0 + r / g.group + 1) : w.n) : 0;
+        lim[i] = r < real ? (g.causal ? max(0, w.q.n - w.q.T + tok0 + r / g.group + 1) : w.q.n) : 0;
       }
-      const int most = attend_limit(cs, g, as, w.s, w.n, w.at.b);
-      const int least = g.causal ? max(0, w.n - w.T + tok0 + 1) : w.n;
+      const int most = w.limit;
+      const int least = g.causal ? max(0, w.q.n - w.q.T + tok0 + 1) : w.q.n;
       float acc[16][4];
 #pragma unroll
       for (int i = 0; i < 16; ++i)
@@ -331,8 +320,8 @@ attend_rows_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, cons
         }
         if (whole) {
           const int t = r / g.group, h = w.at.h * g.group + r - t * g.group;
-          const int64_t tok = cs.new_off[w.s] + tok0 + t;
-          const bool none = (g.causal ? w.n - w.T + tok0 + t + 1 : w.n) <= 0;       // no key
+          const int64_t tok = w.q.row0 + tok0 + t;
+          const bool none = (g.causal ? w.q.n - w.q.T + tok0 + t + 1 : w.q.n) <= 0;       // no key
           const float inv = none ? 0.f : 1.0f / total;
           *reinterpret_cast<uint2*>(o.out + tok * g.out_tok + h * g.out_head + c) =
               make_uint2(pack_bf16(v.x * inv, v.y * inv), pack_bf16(v.z * inv, v.w * inv));
@@ -355,11 +344,11 @@ attend_rows_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, cons
 
 }  // namespace
 
-cudaError_t launch_attend_rows(const Launch& L, const CacheSeqs& cs, const CacheGeom& g, const AttendSeqs& as, const AttendWs& ws,
+cudaError_t launch_attend_rows(const Launch& L, const CacheGeom& g, const AttendSeqs& as, const AttendWs& ws,
                                int grid, const AttendOut& o, const void* q, const CUtensorMap& k_map, const CUtensorMap& v_map) {
   const cudaError_t e = allow_smem(attend_rows_kernel);
   if (e != cudaSuccess) return e;
-  return launch_pdl(attend_rows_kernel, dim3((unsigned)grid), dim3(kThreads), kSmem, L.stream, 1, cs, g, as, k_map, v_map,
+  return launch_pdl(attend_rows_kernel, dim3((unsigned)grid), dim3(kThreads), kSmem, L.stream, 1, g, as, k_map, v_map,
                     (const uint16_t*)q, o, ws, L.status);
 }
 

@@ -59,12 +59,10 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return r;
 }
 
-// 2^(v c + off) of 32 values, as bf16 to tensor memory and added to `sum`; POLY: some on the FMA pipe, whose largest value goes
-// into `reach`.
+// 2^(v c + off) of 32 values as bf16, added to `sum`; POLY: some on the FMA pipe, whose largest value goes into `reach`.
 template <bool POLY>
-__device__ __forceinline__ void exponentials(const uint32_t (&v)[32], uint64_t c2, uint64_t off2, uint32_t p_addr, uint64_t (&sum)[2],
+__device__ __forceinline__ void exponentials(const uint32_t (&v)[32], uint64_t c2, uint64_t off2, uint32_t (&p)[16], uint64_t (&sum)[2],
                                              float& reach) {
-  uint32_t p[16];
 #pragma unroll
   for (int e = 0; e < 16; ++e) {
     const float a = __uint_as_float(v[2 * e]), b = __uint_as_float(v[2 * e + 1]);
@@ -77,7 +75,6 @@ __device__ __forceinline__ void exponentials(const uint32_t (&v)[32], uint64_t c
     unpack2(y, y0, y1);
     p[e] = pack_bf16(y0, y1);
   }
-  tmem_st16(p_addr, p);
 }
 __device__ __forceinline__ float total_of(const uint64_t (&sum)[2]) {
   float a, b;
@@ -135,7 +132,7 @@ __device__ __forceinline__ void hand_over(uint32_t bar, int lane) {
 }
 
 __global__ void __launch_bounds__(kThreads, 1)
-attend_tc_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, const __grid_constant__ AttendSeqs as,
+attend_tc_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
                  const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
                  const __grid_constant__ CUtensorMap v_map, const AttendOut o, const AttendWs ws, DeviceStatus* status) {
   extern __shared__ uint8_t dyn[];
@@ -144,6 +141,11 @@ attend_tc_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, const 
   Shared* sh = reinterpret_cast<Shared*>(ring + (size_t)kStages * kTileBytes);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_launch_dependents();
+  if (warp == kTmaWarp && elect_one()) {
+    prefetch_map(&q_map);
+    prefetch_map(&k_map);
+    prefetch_map(&v_map);
+  }
   if (warp == kMmaWarp) {
     if (lane < kStages) {
       mbar_init(smem_u32(&sh->full[lane]), 1);
@@ -167,24 +169,9 @@ attend_tc_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, const 
     tmem_alloc(smem_u32(&sh->tmem_base), 512);
     tmem_relinquish();
   }
-  pdl_wait();
-  attend_weigh(cs, g, as, &sh->share, status);
   tc_fence_before();
-  __syncthreads();
+  attend_share(g, as, &sh->share, ws.place, status);         // (synchronises)
   tc_fence_after();
-  const int workers = attend_workers(as, &sh->share, g.hkv, gridDim.x);
-  if (warp < 2) {
-    const Place p = attend_place(cs, g, as, &sh->share, blockIdx.x + warp, workers);
-    if (lane == 0) {
-      if (warp == 0) {
-        sh->share.from = p;
-        ws.place[blockIdx.x] = blockIdx.x < workers ? p : Place{0, 0, 0, -1};
-      } else {
-        sh->share.to = p;
-      }
-    }
-  }
-  __syncthreads();
   const uint32_t tmem = __shfl_sync(0xffffffffu, sh->tmem_base, 0);
   const BoundedWait pipe = {&sh->abort_flag, &status->code};
   auto wait = [&](uint64_t* bar, uint32_t parity, int where) { return bounded_wait(pipe, bar, parity, CC_ERR_TIMEOUT, where); };
@@ -199,11 +186,11 @@ attend_tc_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, const 
     int stage = 0;
     uint32_t phase = 0, q_phase = 0;
     bool ok = true;
-    for (bool more = w.first(cs, g, as, &sh->share); more && ok; more = w.next(cs, g, as, &sh->share)) {
-      const int limit = attend_limit(cs, g, as, w.s, w.n, w.at.b);
-      const int32_t* table = g.table + (int64_t)w.s * g.table_stride;
+    for (bool more = w.first(g, as, &sh->share); more && ok; more = w.next(g, as, &sh->share)) {
+      const int limit = w.limit;
+      const int32_t* table = g.table + (int64_t)as.src[w.at.i] * g.table_stride;
       const int tok0 = w.at.b * as.block_tokens;
-      const bool second = w.T - tok0 > as.tile_tokens;
+      const bool second = w.q.T - tok0 > as.tile_tokens;
       for (int t = w.t0; t < w.t1 && ok; ++t) {
         const int key = t * kTcTile + lane * span;             // first key of this lane's copy
         const bool mine = lane < copies && key < limit;
@@ -232,7 +219,7 @@ attend_tc_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, const 
               const uint32_t qb = smem_u32(&sh->q_full);
               mbar_expect_tx(qb, q_bytes * (second ? 4u : 2u));
               for (int i = 0; i < (second ? 2 : 1); ++i) {
-                const int tok = cs.new_off[w.s] + tok0 + i * as.tile_tokens;
+                const int tok = w.q.row0 + tok0 + i * as.tile_tokens;
                 const uint32_t at = smem_u32(q_smem) + (uint32_t)i * kTileBytes;
                 tma_load_3d(at, &q_map, qb, 0, w.at.h * g.group, tok);
                 tma_load_3d(at + kTileBytes / 2, &q_map, qb, 64, w.at.h * g.group, tok);
@@ -277,9 +264,9 @@ attend_tc_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, const 
       }
     };
     bool ok = true;
-    for (bool more = w.first(cs, g, as, &sh->share); more && ok; more = w.next(cs, g, as, &sh->share)) {
+    for (bool more = w.first(g, as, &sh->share); more && ok; more = w.next(g, as, &sh->share)) {
       if (w.t0 == w.t1) continue;
-      const bool second = w.T - w.at.b * as.block_tokens > as.tile_tokens;
+      const bool second = w.q.T - w.at.b * as.block_tokens > as.tile_tokens;
       const int tiles = second ? 2 : 1;
       ok = wait(&sh->full[stage], phase, 82) && wait(&sh->q_full, q_phase, 83);
       if (!ok) break;
@@ -340,28 +327,28 @@ attend_tc_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, const 
     uint32_t s_phase = 0, of_phase = 0;
     uint32_t entry = 1;                            // of V of the next tile in the order of the ring
     bool dead = false;
-    for (bool more = w.first(cs, g, as, &sh->share); more; more = w.next(cs, g, as, &sh->share)) {
+    for (bool more = w.first(g, as, &sh->share); more; more = w.next(g, as, &sh->share)) {
       const int tok = w.at.b * as.block_tokens + i * as.tile_tokens + in_tile;       // of the sequence
-      if (w.T - w.at.b * as.block_tokens <= i * as.tile_tokens) {                    // no such tile
+      if (w.q.T - w.at.b * as.block_tokens <= i * as.tile_tokens) {                    // no such tile
         entry += 2u * (uint32_t)(w.t1 - w.t0);
         continue;
       }
-      const bool real = in_tile < as.tile_tokens && tok < w.T;
-      const int lim = real ? (g.causal ? max(0, w.n - w.T + tok + 1) : w.n) : 0;     // keys that the row attends to
-      const int most = attend_limit(cs, g, as, w.s, w.n, w.at.b);
+      const bool real = in_tile < as.tile_tokens && tok < w.q.T;
+      const int lim = real ? (g.causal ? max(0, w.q.n - w.q.T + tok + 1) : w.q.n) : 0;     // keys that the row attends to
       const bool idle = !__any_sync(0xffffffffu, real);
       const int least = __reduce_min_sync(0xffffffffu, real ? lim : 0x7fffffff);
+      const int plain = min(least, w.limit) / kTcTile;         // tiles before this one have no masked keys
       float ref = -INFINITY;
       uint64_t sum[2] = {0ull, 0ull};
       for (int t = w.t0; t < w.t1; ++t, entry += 2) {
         if (!dead) dead = !wait(&sh->s_full[i], s_phase, 88 + i);
         s_phase ^= 1;
         const int key0 = t * kTcTile;
-        if (!dead && i == 0 && key0 + kTcTile > most) {
+        if (t >= plain && !dead && i == 0 && key0 + kTcTile > w.limit) {
           // rows of V that no row of the block attends to may hold anything: 0 x NaN.  (Both products with V wait for this tile's P.)
           const int stage = entry % kStages;
           dead = !wait(&sh->full[stage], (entry / kStages) & 1, 90);
-          for (int e = (most - key0) * 16 + (int)threadIdx.x; e < kTcTile * 16; e += 128)
+          for (int e = (w.limit - key0) * 16 + (int)threadIdx.x; e < kTcTile * 16; e += 128)
             *reinterpret_cast<uint4*>(ring + (size_t)stage * kTileBytes + (e >> 7) * 2048 + ((e >> 3) & 1) * 1024 +
                                       ((e >> 4) & 7) * 128 + (e & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
           fence_proxy_async();
@@ -370,49 +357,47 @@ attend_tc_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, const 
         if (!dead && !idle) {
           const uint32_t p_bar = smem_u32(&sh->p_full[i][0]);
           int from = 0;                            // first chunk of 32 keys that is not handed over yet
-          if (t > w.t0 && key0 + kTcTile <= least) {
-            // With the reference that there is.  P of a half goes over the first columns of S, of which chunk 0 is still in
-            // registers when the half is checked, and goes back if it has to be computed again.
-            uint32_t v0[32], v1[32];
+          if (t > w.t0 && t < plain) {
+            // With the reference that there is.
+            uint32_t v0[32], v1[32], p0[16], p1[16];
             float reach = -INFINITY;
             uint64_t part[2] = {0ull, 0ull};
             const uint64_t off2 = offset_of(ref);
             tmem_ld32(s_addr, v0);
-            tmem_wait_ld();
             tmem_ld32(s_addr + 32, v1);
-            exponentials<true>(v0, c22, off2, s_addr, part, reach);
             tmem_wait_ld();
-            exponentials<true>(v1, c22, off2, s_addr + 16, part, reach);
-            if (out_of_range(real, part, reach, c2, ref)) {
-              tmem_st32(s_addr, v0);
-              tmem_wait_st();
-            } else {
+            exponentials<true>(v0, c22, off2, p0, part, reach);
+            exponentials<true>(v1, c22, off2, p1, part, reach);
+            if (!out_of_range(real, part, reach, c2, ref)) {
+              tmem_st16(s_addr, p0);
+              tmem_st16(s_addr + 16, p1);
+              tmem_ld32(s_addr + 64, v0);
+              tmem_ld32(s_addr + 96, v1);
               hand_over(p_bar, lane);
               from = 2;
               sum[0] = add2(sum[0], part[0]);
               sum[1] = add2(sum[1], part[1]);
               part[0] = part[1] = 0ull;
               reach = -INFINITY;
-              tmem_ld32(s_addr + 64, v0);
               tmem_wait_ld();
-              tmem_ld32(s_addr + 96, v1);
-              exponentials<true>(v0, c22, off2, s_addr + 32, part, reach);
-              tmem_wait_ld();
-              exponentials<true>(v1, c22, off2, s_addr + 48, part, reach);
-              if (out_of_range(real, part, reach, c2, ref)) {
-                dead = !wait(&sh->half_done[i], s_phase ^ 1, 92);        // the product of the first half with V is under way
-                tc_fence_after();
-              } else {
+              exponentials<true>(v0, c22, off2, p0, part, reach);
+              exponentials<true>(v1, c22, off2, p1, part, reach);
+              if (!out_of_range(real, part, reach, c2, ref)) {
+                tmem_st16(s_addr + 32, p0);
+                tmem_st16(s_addr + 48, p1);
                 hand_over(p_bar + 8, lane);
                 from = 4;
                 sum[0] = add2(sum[0], part[0]);
                 sum[1] = add2(sum[1], part[1]);
+              } else {
+                dead = !wait(&sh->half_done[i], s_phase ^ 1, 92);        // the product of the first half with V is under way
+                tc_fence_after();
               }
             }
           }
           if (from < 4) {
             // The maximum first: the first tile of a row, tiles with masked keys, logits far above the reference.
-            const int last = key0 + kTcTile > least ? lim - key0 : kTcTile;
+            const int last = t >= plain ? lim - key0 : kTcTile;
             float high = -INFINITY;
             uint32_t v[32];
 #pragma unroll 1
@@ -438,7 +423,9 @@ attend_tc_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, const 
                 for (int e = 0; e < 32; ++e)
                   if (c * 32 + e >= last) v[e] = 0xff800000u;
               }
-              exponentials<false>(v, c22, off2, s_addr + c * 16, sum, reach);
+              uint32_t p[16];
+              exponentials<false>(v, c22, off2, p, sum, reach);
+              tmem_st16(s_addr + c * 16, p);
               if (c & 1) hand_over(p_bar + (c >> 1) * 8, lane);
             }
           }
@@ -458,7 +445,7 @@ attend_tc_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, const 
       const float total = total_of(sum);
       const bool whole = w.whole();
       const int h = w.at.h * g.group + r - in_tile * g.group;
-      const int64_t row = cs.new_off[w.s] + tok, at = (int64_t)w.slot() * as.rows + i * 128 + r;
+      const int64_t row = w.q.row0 + tok, at = (int64_t)w.slot() * as.rows + i * 128 + r;
       if (!dead && !idle) {
         const float inv = lim <= 0 ? 0.f : 1.0f / total;
         if (real && whole && o.lse) o.lse[row * g.hq + h] = lim <= 0 ? -INFINITY : (ref + log2f(total)) * kLn2;
@@ -514,12 +501,12 @@ attend_tc_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, const 
 
 }  // namespace
 
-cudaError_t launch_attend_tc(const Launch& L, const CacheSeqs& cs, const CacheGeom& g, const AttendSeqs& as, const AttendWs& ws,
+cudaError_t launch_attend_tc(const Launch& L, const CacheGeom& g, const AttendSeqs& as, const AttendWs& ws,
                              int grid, const AttendOut& o, const CUtensorMap& q_map, const CUtensorMap& k_map,
                              const CUtensorMap& v_map) {
   const cudaError_t e = allow_smem(attend_tc_kernel);
   if (e != cudaSuccess) return e;
-  return launch_pdl(attend_tc_kernel, dim3((unsigned)grid), dim3(kThreads), kSmem, L.stream, 1, cs, g, as, q_map, k_map, v_map,
+  return launch_pdl(attend_tc_kernel, dim3((unsigned)grid), dim3(kThreads), kSmem, L.stream, 1, g, as, q_map, k_map, v_map,
                     o, ws, L.status);
 }
 

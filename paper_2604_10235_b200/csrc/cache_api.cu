@@ -171,8 +171,10 @@ size_t cc_attention_workspace_bytes(const cc_ctx* ctx, const cc_cache_desc* desc
   CacheSeqs cs;
   CacheGeom g;
   if (take_desc(const_cast<cc_ctx*>(ctx), desc, &cs, &g) != CC_OK) return 0;
+  if (cs.new_off[cs.num_seqs] == 0) return 256;
   const size_t n = align256(attend_ws_bytes(cs, g, ctx->sm_count));
-  return n > 256 ? n : 256;
+  if (n == 0) fail(const_cast<cc_ctx*>(ctx), CC_ERR_UNSUPPORTED, "2^31 tiles of work and more in one call");
+  return n;
 }
 
 int cc_paged_attention(cc_ctx* ctx, const cc_cache_desc* desc, const void* q, const void* k, const void* v, void* out,
@@ -186,7 +188,9 @@ int cc_paged_attention(cc_ctx* ctx, const cc_cache_desc* desc, const void* q, co
   if (cs.new_off[cs.num_seqs] == 0) return CC_OK;
   if (!q || !k || !v || !out) return fail(ctx, CC_ERR_INVALID_ARG, "NULL tensor pointer");
   if (!aligned({q, k, v, out})) return fail(ctx, CC_ERR_INVALID_ARG, "tensor pointers must be 16-byte aligned");
-  if ((rc = check_ws(ctx, attend_ws_bytes(cs, g, ctx->sm_count), ws, ws_bytes)) != CC_OK) return rc;
+  const size_t need = attend_ws_bytes(cs, g, ctx->sm_count);
+  if (need == 0) return fail(ctx, CC_ERR_UNSUPPORTED, "2^31 tiles of work and more in one call");
+  if ((rc = check_ws(ctx, need, ws, ws_bytes)) != CC_OK) return rc;
   const DeviceScope scope(ctx->device);
   if (scope.error != cudaSuccess) return cuda_fail(ctx, scope.error, "context's device");
   int drv = 0;

@@ -67,7 +67,7 @@ struct ForkArgs {
 static_assert(CC_MAX_SEQS <= 256, "parents in a byte");
 cudaError_t launch_fork(const Launch& L, const CacheSeqs& cs, const CacheGeom& g, const ForkArgs& a);
 
-// Attention: bytes of workspace; launch (drv_err receives the code of a failed tensor map).
+// Attention: bytes of workspace (0: more work than a call takes); launch (drv_err receives the code of a failed tensor map).
 size_t attend_ws_bytes(const CacheSeqs& cs, const CacheGeom& g, int sm_count);
 cudaError_t launch_attend(const Launch& L, const CacheSeqs& cs, const CacheGeom& g, const void* q, const void* k, const void* v,
                           void* out, float* lse, void* ws, void* encode_fn, int* drv_err);

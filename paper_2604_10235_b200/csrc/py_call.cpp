@@ -9,6 +9,10 @@
 //   p  a CUDA or page-locked host tensor, or None
 //   w  a CUDA tensor as two words: address, number of elements
 //   L  a sequence of tensors as a host array of addresses, or None
+//   d  a device number (no word): the tensors of the kinds below are on that device
+//   b, n, f  a CUDA tensor of bfloat16, int32, float32, or None
+//   M  a sequence of bfloat16 tensors as a host array of addresses
+//   h  a contiguous host array (numpy) of 32-bit integers
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <stdint.h>
@@ -25,7 +29,8 @@ namespace {
 
 constexpr int kMaxWords = 20;
 
-PyObject *s_data_ptr, *s_is_cuda, *s_is_pinned, *s_numel;
+PyObject *s_data_ptr, *s_is_cuda, *s_is_pinned, *s_numel, *s_dtype, *s_get_device;
+PyObject *t_bf16, *t_i32, *t_f32;      // torch's types, looked up with the first spec that names one
 
 bool word_of(PyObject* o, uint64_t* out) {
   *out = PyLong_AsUnsignedLongLongMask(o);
@@ -62,6 +67,35 @@ bool tensor_word(PyObject* o, bool pinned_ok, uint64_t* out) {
     }
   }
   return word_from(o, s_data_ptr, out);
+}
+
+// A tensor of the given type on the given device, or None where that is allowed.
+bool typed_word(PyObject* o, PyObject* dtype, long device, bool none_ok, uint64_t* out) {
+  if (none_ok && o == Py_None) {
+    *out = 0;
+    return true;
+  }
+  PyObject* t = PyObject_GetAttr(o, s_dtype);
+  if (!t) return false;
+  const bool same = t == dtype;
+  Py_DECREF(t);
+  uint64_t at = 0;
+  if (same && !word_from(o, s_get_device, &at)) return false;
+  if (!same || (long)at != device) {
+    PyErr_Format(PyExc_ValueError, "libcodecomp takes a tensor of %S on cuda:%ld here", dtype, device);
+    return false;
+  }
+  return word_from(o, s_data_ptr, out);
+}
+
+bool host_word(PyObject* o, uint64_t* out) {
+  Py_buffer view;
+  if (PyObject_GetBuffer(o, &view, PyBUF_C_CONTIGUOUS) != 0) return false;
+  const bool ok = view.itemsize == 4;
+  *out = (uint64_t)(uintptr_t)view.buf;            // (the caller's array outlives the call)
+  PyBuffer_Release(&view);
+  if (!ok) PyErr_SetString(PyExc_ValueError, "an array of 32-bit integers is needed");
+  return ok;
 }
 
 template <class T>
@@ -112,6 +146,7 @@ PyObject* call_bound(PyObject* self, PyObject* const* args, Py_ssize_t n_args) {
   uint64_t a[kMaxWords];
   std::vector<std::vector<uint64_t>> lists;      // host arrays of the call (moving the outer one keeps their storage)
   int n = 0;
+  long device = -1;
   for (Py_ssize_t i = 0; i < n_args; ++i) {
     PyObject* o = args[i];
     bool ok = true;
@@ -120,13 +155,26 @@ PyObject* call_bound(PyObject* self, PyObject* const* args, Py_ssize_t n_args) {
       case 't': ok = tensor_word(o, false, &a[n++]); break;
       case 'p': ok = tensor_word(o, true, &a[n++]); break;
       case 'w': ok = tensor_word(o, false, &a[n]) && word_from(o, s_numel, &a[n + 1]); n += 2; break;
+      case 'd':
+        device = PyLong_AsLong(o);
+        ok = !(device == -1 && PyErr_Occurred());
+        break;
+      case 'b': ok = typed_word(o, t_bf16, device, true, &a[n++]); break;
+      case 'n': ok = typed_word(o, t_i32, device, true, &a[n++]); break;
+      case 'f': ok = typed_word(o, t_f32, device, true, &a[n++]); break;
+      case 'h': ok = host_word(o, &a[n++]); break;
+      case 'M':
       case 'L': {
-        if (o == Py_None) { a[n++] = 0; break; }
+        if (o == Py_None && f->spec[i] == 'L') { a[n++] = 0; break; }
         PyObject* seq = PySequence_Fast(o, "a sequence of tensors");
         if (!seq) return nullptr;
         const Py_ssize_t m = PySequence_Fast_GET_SIZE(seq);
         lists.emplace_back((size_t)m + 1);
-        for (Py_ssize_t j = 0; j < m && ok; ++j) ok = word_from(PySequence_Fast_GET_ITEM(seq, j), s_data_ptr, &lists.back()[j]);
+        for (Py_ssize_t j = 0; j < m && ok; ++j) {
+          PyObject* item = PySequence_Fast_GET_ITEM(seq, j);
+          ok = f->spec[i] == 'L' ? word_from(item, s_data_ptr, &lists.back()[j])
+                                 : typed_word(item, t_bf16, device, false, &lists.back()[j]);
+        }
         Py_DECREF(seq);
         a[n++] = (uint64_t)(uintptr_t)lists.back().data();
         break;
@@ -161,10 +209,20 @@ PyObject* bind(PyObject*, PyObject* args) {
   for (const Entry& e : kEntries)
     if (strcmp(e.name, name) == 0) entry = &e;
   if (!entry) return PyErr_Format(PyExc_ValueError, "%s cannot be bound", name);
+  if (len > kMaxWords) return PyErr_Format(PyExc_ValueError, "the spec of %s is too long", name);
   int words = 0;
   for (Py_ssize_t i = 0; i < len; ++i) {
-    if (!spec[i] || !strchr("itpwL", spec[i])) return PyErr_Format(PyExc_ValueError, "unknown kind of argument in the spec of %s", name);
-    words += spec[i] == 'w' ? 2 : 1;
+    if (!spec[i] || !strchr("itpwLdbnfMh", spec[i])) return PyErr_Format(PyExc_ValueError, "unknown kind of argument in the spec of %s", name);
+    words += spec[i] == 'w' ? 2 : spec[i] == 'd' ? 0 : 1;
+    if (strchr("bnfM", spec[i]) && !t_f32) {
+      PyObject* torch = PyImport_ImportModule("torch");
+      if (!torch) return nullptr;
+      t_bf16 = PyObject_GetAttrString(torch, "bfloat16");
+      t_i32 = PyObject_GetAttrString(torch, "int32");
+      t_f32 = PyObject_GetAttrString(torch, "float32");
+      Py_DECREF(torch);
+      if (!t_bf16 || !t_i32 || !t_f32) return nullptr;
+    }
   }
   if (words != entry->words) return PyErr_Format(PyExc_ValueError, "%s takes %d words, its spec gives %d", name, entry->words, words);
   Bound* f = new (std::nothrow) Bound{entry, reinterpret_cast<void*>((uintptr_t)fn), (int)len, {}};
@@ -192,5 +250,7 @@ PyMODINIT_FUNC PyInit__cccall(void) {
   s_is_cuda = PyUnicode_InternFromString("is_cuda");
   s_is_pinned = PyUnicode_InternFromString("is_pinned");
   s_numel = PyUnicode_InternFromString("numel");
+  s_dtype = PyUnicode_InternFromString("dtype");
+  s_get_device = PyUnicode_InternFromString("get_device");
   return PyModule_Create(&module);
 }

@@ -180,3 +180,43 @@ def test_binding_struct_matches_header_field_order():
             words_ = [w for w in decl.replace("*", " ").split() if w not in ("const", "int32_t", "int64_t", "uint64_t", "float", "double")]
             fields += [f.strip() for f in " ".join(words_).split(",") if f.strip()]
         assert fields == [f[0] for f in struct._fields_]
+
+
+def test_too_much_work_for_one_call_is_refused():
+    c = Call((2 ** 30, 2 ** 30), (2 ** 29, 2 ** 29))
+    c.d.n_heads_q, c.d.n_heads_kv, c.d.page_table_stride = 64, 1, 2 ** 26
+    c.ctx = C.create_string_buffer(bytes(4) + (148).to_bytes(4, "little") + bytes(4088), 4096)
+    assert c.lib.cc_attention_workspace_bytes(c.ctx, C.byref(c.d)) == 0
+    assert c.attend() == cc.CC_ERR_UNSUPPORTED and "tiles" in c.text
+
+
+def test_typed_arguments_are_checked():
+    """bfloat16 tensors of the context's device; what is on the host is on device -1, which stands for any other here."""
+    import torch
+    call = Call()
+    lib, at = call.lib, C.addressof(call.ctx)
+    bf, f32, i32 = torch.zeros(4, dtype=torch.bfloat16), torch.zeros(4), torch.zeros(4, dtype=torch.int32)
+    attend = lib.calls["cc_paged_attention"]
+    desc = C.addressof(call.d)
+    for args in ((f32, bf, bf, bf, f32), (bf, i32, bf, bf, f32), (bf, bf, bf, bf, bf)):
+        with pytest.raises(ValueError):
+            attend(at, desc, -1, *args, None, 0)
+    with pytest.raises(ValueError):
+        attend(at, desc, 0, bf, bf, bf, bf, f32, None, 0)
+    with pytest.raises(AttributeError):
+        attend(at, desc, -1, object(), bf, bf, bf, f32, None, 0)
+    rope = lib.calls["cc_rope_append"]
+    assert rope(at, desc, -1, None, None, None, None, None, None, None, 0) == cc.CC_OK
+    with pytest.raises(ValueError):
+        rope(at, desc, -1, None, None, None, f32, None, None, None, 0)
+    fork = lib.calls["cc_fork_pages"]
+    parents = np.array([0, 5], np.int32)
+    assert fork(at, desc, -1, 0, [], [], parents, 2, i32, 3, i32, 0) == cc.CC_OK
+    with pytest.raises(ValueError):
+        fork(at, desc, -1, 1, [f32], [bf], parents, 2, i32, 3, i32, 0)
+    with pytest.raises(ValueError):
+        fork(at, desc, -1, 1, [bf], [bf], parents.astype(np.int64), 2, i32, 3, i32, 0)
+    with pytest.raises(AttributeError):
+        fork(at, desc, -1, 1, [None], [bf], parents, 2, i32, 3, i32, 0)
+    with pytest.raises((TypeError, BufferError)):
+        fork(at, desc, -1, 1, [bf], [bf], [0, 5], 2, i32, 3, i32, 0)
