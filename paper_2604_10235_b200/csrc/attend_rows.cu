@@ -34,9 +34,9 @@ constexpr int kFoldPitch = kHeadDim + 8;         // floats of an output row in s
 constexpr float kSlack = 8.0f;                   // log2 of how far a logit may lie above the reference
 
 struct Shared {
-  float fold[4][kRowsMost * kFoldPitch];         // outputs of the warps while they are joined
+  float fold[kWorkers][kRowsMost * kFoldPitch];  // outputs of the warps while they are joined
   uint8_t q[2][kRowsMost * kQPitch];
-  float2 stat[2][kWorkers][kRowsMost];           // (reference, sum) of a problem's rows by warp
+  float2 stat[kWorkers][kRowsMost];              // (reference, sum) of a problem's rows by warp
   AttendShare share;
   uint64_t full[kStages], empty[kStages], q_full[2], q_empty[2];
   int abort_flag;
@@ -115,6 +115,12 @@ attend_rows_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
     uint32_t phase = 0;
     bool ok = true;
     for (bool more = w.first(g, as, &sh->share); more && ok; more = w.next(g, as, &sh->share), ++seg) {
+      const int32_t* table = g.table + (int64_t)as.src[w.at.i] * g.table_stride;
+      auto page_of = [&](int t) {                  // of this lane's copy, -1 where it has none
+        const int key = t * kRowsTile + lane * span;
+        return lane < copies && key < w.limit && t < w.t1 ? table[key >> g.page_shift] : -1;
+      };
+      int page = page_of(w.t0);                    // always one tile ahead
       const int buf = seg & 1;
       if (!bounded_wait(pipe, &sh->q_empty[buf], ((seg >> 1) & 1) ^ 1, CC_ERR_TIMEOUT, 70)) break;
       const int rows = min(as.block_tokens, w.q.T - w.at.b * as.block_tokens) * g.group;
@@ -126,19 +132,17 @@ attend_rows_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
         const int64_t tok = w.q.row0 + w.at.b * as.block_tokens + t;
         bulk_load(smem_u32(sh->q[buf]) + lane * kQPitch, q + tok * g.q_tok + h * g.q_head, kHeadDim * 2, qb);
       }
-      const int limit = w.limit;
-      const int32_t* table = g.table + (int64_t)as.src[w.at.i] * g.table_stride;
       for (int t = w.t0; t < w.t1; ++t) {
         const int key = t * kRowsTile + lane * span;           // first key of this lane's copy
-        const bool mine = lane < copies && key < limit;
-        int page = -1;
-        if (mine) page = table[key >> g.page_shift];
+        const bool mine = lane < copies && key < w.limit;
+        const int id = page;
+        page = page_of(t + 1);
         if (!bounded_wait(pipe, &sh->empty[stage], phase ^ 1, CC_ERR_TIMEOUT, 71)) { ok = false; break; }
-        const bool good = mine && page >= 0 && page < g.pool_pages;
+        const bool good = mine && id >= 0 && id < g.pool_pages;
         if (mine && !good) report_error(status, CC_ERR_DEVICE_FLAG, 620);
         const unsigned mask = __ballot_sync(0xffffffffu, good);
         // first group of eight rows of the copy
-        const int group8 = (int)((((int64_t)page << g.page_shift) + (key & ((1 << g.page_shift) - 1))) >> 3);
+        const int group8 = (int)((((int64_t)id << g.page_shift) + (key & ((1 << g.page_shift) - 1))) >> 3);
         const uint32_t fb = smem_u32(&sh->full[stage]);
         const uint32_t dst = smem_u32(ring) + (uint32_t)stage * 2 * kTileBytes;
         if (elected) mbar_expect_tx(fb, (uint32_t)__popc(mask) * 2u * copy_bytes);
@@ -270,53 +274,37 @@ attend_rows_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
         sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 1);
         sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], 2);
       }
-      if ((lane & 3) < 2) sh->stat[buf][me][r0 + 8 * (lane & 1)] = make_float2(lane & 1 ? ref[1] : ref[0], lane & 1 ? sum[1] : sum[0]);
-      worker_barrier();
-      float f[2];
+      if (seg > 0) worker_barrier();               // what the warps left of the problem before has been read
+      if ((lane & 3) < 2) sh->stat[me][r0 + 8 * (lane & 1)] = make_float2(lane & 1 ? ref[1] : ref[0], lane & 1 ? sum[1] : sum[0]);
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        float top = -INFINITY;
-#pragma unroll
-        for (int k = 0; k < kWorkers; ++k) top = fmaxf(top, sh->stat[buf][k][r0 + 8 * i].x);
-        f[i] = ref[i] == -INFINITY ? 0.f : ex2(ref[i] - top);
-      }
-      float* fold = sh->fold[quarter];
-      if (group == 1) {
+        if (8 * i >= real) break;
 #pragma unroll
         for (int c = 0; c < 16; ++c)
-#pragma unroll
-          for (int i = 0; i < 2; ++i)
-            *reinterpret_cast<float2*>(fold + (r0 + 8 * i) * kFoldPitch + c * 8 + 2 * (lane & 3)) =
-                make_float2(acc[c][2 * i] * f[i], acc[c][2 * i + 1] * f[i]);
-      }
-      worker_barrier();
-      if (group == 0) {
-#pragma unroll
-        for (int c = 0; c < 16; ++c)
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {
-            float2* at = reinterpret_cast<float2*>(fold + (r0 + 8 * i) * kFoldPitch + c * 8 + 2 * (lane & 3));
-            const float2 other = *at;
-            *at = make_float2(acc[c][2 * i] * f[i] + other.x, acc[c][2 * i + 1] * f[i] + other.y);
-          }
+          *reinterpret_cast<float2*>(sh->fold[me] + (r0 + 8 * i) * kFoldPitch + c * 8 + 2 * (lane & 3)) =
+              make_float2(acc[c][2 * i], acc[c][2 * i + 1]);
       }
       worker_barrier();
       const bool whole = w.whole();
       for (int i = threadIdx.x - 32; i < real * 32; i += kWorkers * 32) {
         const int r = i >> 5, c = (i & 31) * 4;
+        float2 st[kWorkers];
         float top = -INFINITY, total = 0.f;
 #pragma unroll
-        for (int k = 0; k < kWorkers; ++k) top = fmaxf(top, sh->stat[buf][k][r].x);
-#pragma unroll
         for (int k = 0; k < kWorkers; ++k) {
-          const float2 st = sh->stat[buf][k][r];
-          total += st.y * (st.x == -INFINITY ? 0.f : ex2(st.x - top));
+          st[k] = sh->stat[k][r];
+          top = fmaxf(top, st[k].x);
         }
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
+        for (int k = 0; k < kWorkers; ++k) {
+          const float f = st[k].x == -INFINITY ? 0.f : ex2(st[k].x - top);
+          total = fmaf(st[k].y, f, total);
           const float4 part = *reinterpret_cast<const float4*>(sh->fold[k] + r * kFoldPitch + c);
-          v.x += part.x; v.y += part.y; v.z += part.z; v.w += part.w;
+          v.x = fmaf(part.x, f, v.x);
+          v.y = fmaf(part.y, f, v.y);
+          v.z = fmaf(part.z, f, v.z);
+          v.w = fmaf(part.w, f, v.w);
         }
         if (whole) {
           const int t = r / g.group, h = w.at.h * g.group + r - t * g.group;

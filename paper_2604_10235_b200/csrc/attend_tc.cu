@@ -14,7 +14,8 @@
 // P up to 1.  So only the first tile of a row and masked ones look at their maximum beforehand, the others compute with
 // the reference that there is; where the sum of a half tile shows that a logit is far above it (or no number), nothing has been
 // handed over yet, the row's maximum becomes the reference, its O is scaled in tensor memory and the half is computed again.
-// One pair of exponentials in four is evaluated on the FMA pipe (exp2_poly.cuh), for the special-function unit is the fuller one.
+// One pair of exponentials in eight is evaluated on the FMA pipe (exp2_poly.cuh): 2048 x 32768 1057 us with one in four, 1054 with one in
+// eight, 1077 with one in sixteen; 517 x 8709 96.3, 94.1, 94.7.
 //
 // Roles (320 threads, one CTA per SM): warps 0-3 and 4-7 the softmax of the two tiles, warp 8 the copies (Q once per
 // problem, K and V by turns through a ring of five stages of 32 KB, a copy per page), warp 9 the products.
@@ -67,7 +68,7 @@ __device__ __forceinline__ void exponentials(const uint32_t (&v)[32], uint64_t c
   for (int e = 0; e < 16; ++e) {
     const float a = __uint_as_float(v[2 * e]), b = __uint_as_float(v[2 * e + 1]);
     const uint64_t x = fma2(pack2(a, b), c2, off2);
-    const bool poly = POLY && e % 4 == 3;
+    const bool poly = POLY && e % 8 == 7;
     const uint64_t y = poly ? ex2_pair_fma(x) : ex2_pair_sfu(x);
     if (poly) reach = max3_nan(reach, a, b);
     sum[e & 1] = add2(sum[e & 1], y);
@@ -240,77 +241,77 @@ attend_tc_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
     const uint32_t idesc_o = instr_desc(128, 128) | (1u << 16);                            // V: MN-major
     const bool elected = elect_one();
     int stage = 0;
-    uint32_t phase = 0, q_phase = 0, p_phase[2] = {0, 0}, oe_phase[2] = {1, 1};
+    uint32_t phase = 0, q_phase = 0, p_phases = 0, o_phases = 3;         // (of the barriers of both tiles: a bit each)
     auto next_stage = [&] { if (++stage == kStages) { stage = 0; phase ^= 1; } };
     auto scores = [&](int i, uint32_t k_lo) {
-      if (elected) {
 #pragma unroll
-        for (int ks = 0; ks < kHeadDim / 16; ++ks) {
-          const uint32_t a = q_lo + (uint32_t)i * (kTileBytes >> 4) + (ks >= 4 ? (kTileBytes / 2) >> 4 : 0u) + (ks & 3) * 2u;
-          const uint32_t b = k_lo + (1u << 16) + (ks >= 4 ? 1024u >> 4 : 0u) + (ks & 3) * 2u;
-          umma(tmem + i * 128, a | ((uint64_t)q_hi << 32), b | ((uint64_t)r_hi << 32), idesc_s, ks > 0);
-        }
-        umma_commit(smem_u32(&sh->s_full[i]));
+      for (int ks = 0; ks < kHeadDim / 16; ++ks) {
+        const uint32_t a = q_lo + (uint32_t)i * (kTileBytes >> 4) + (ks >= 4 ? (kTileBytes / 2) >> 4 : 0u) + (ks & 3) * 2u;
+        const uint32_t b = k_lo + (1u << 16) + (ks >= 4 ? 1024u >> 4 : 0u) + (ks & 3) * 2u;
+        umma(tmem + i * 128, a | ((uint64_t)q_hi << 32), b | ((uint64_t)r_hi << 32), idesc_s, ks > 0);
       }
+      umma_commit(smem_u32(&sh->s_full[i]));
     };
     auto outputs = [&](int i, int half, uint32_t v_lo, bool accumulate) {
-      if (elected) {
 #pragma unroll
-        for (int s4 = 0; s4 < kTcTile / 32; ++s4) {
-          const int ks = half * (kTcTile / 32) + s4;
-          const uint32_t b = v_lo + ((1024u >> 4) << 16) + ks * (4096u >> 4);
-          umma_tmem_a(tmem + 256 + i * 128, tmem + i * 128 + ks * 8, b | ((uint64_t)r_hi << 32), idesc_o, accumulate || ks > 0);
-        }
+      for (int s4 = 0; s4 < kTcTile / 32; ++s4) {
+        const int ks = half * (kTcTile / 32) + s4;
+        const uint32_t b = v_lo + ((1024u >> 4) << 16) + ks * (4096u >> 4);
+        umma_tmem_a(tmem + 256 + i * 128, tmem + i * 128 + ks * 8, b | ((uint64_t)r_hi << 32), idesc_o, accumulate || ks > 0);
       }
     };
     bool ok = true;
     for (bool more = w.first(g, as, &sh->share); more && ok; more = w.next(g, as, &sh->share)) {
       if (w.t0 == w.t1) continue;
-      const bool second = w.q.T - w.at.b * as.block_tokens > as.tile_tokens;
-      const int tiles = second ? 2 : 1;
+      const int tiles = w.q.T - w.at.b * as.block_tokens > as.tile_tokens ? 2 : 1;
       ok = wait(&sh->full[stage], phase, 82) && wait(&sh->q_full, q_phase, 83);
       if (!ok) break;
       q_phase ^= 1;
       tc_fence_after();
-      for (int i = 0; i < tiles; ++i) scores(i, r_lo + (uint32_t)stage * (kTileBytes >> 4));
-      if (elected) umma_commit(smem_u32(&sh->empty[stage]));
-      if (w.t0 + 1 == w.t1 && elected) umma_commit(smem_u32(&sh->q_empty));
+      if (elected) {
+        for (int i = 0; i < tiles; ++i) scores(i, r_lo + (uint32_t)stage * (kTileBytes >> 4));
+        umma_commit(smem_u32(&sh->empty[stage]));
+        if (w.t0 + 1 == w.t1) umma_commit(smem_u32(&sh->q_empty));
+      }
       next_stage();
       for (int t = w.t0; t < w.t1 && ok; ++t) {
+        const bool more_keys = t + 1 < w.t1;
         const int v_stage = stage;
         ok = wait(&sh->full[stage], phase, 84);
         next_stage();
-        const bool more_keys = t + 1 < w.t1;
         const int k_stage = stage;
-        for (int i = 0; i < tiles && ok; ++i) {
+        if (ok && more_keys) ok = wait(&sh->full[stage], phase, 87);         // (here, not between the products)
+        const uint32_t v_lo = r_lo + (uint32_t)v_stage * (kTileBytes >> 4), k_lo = r_lo + (uint32_t)k_stage * (kTileBytes >> 4);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if (i >= tiles) break;
           if (t == w.t0) {
-            ok = wait(&sh->o_empty[i], oe_phase[i], 85);
-            oe_phase[i] ^= 1;
+            ok = ok && wait(&sh->o_empty[i], (o_phases >> i) & 1, 85);
+            o_phases ^= 1u << i;
           }
-          ok = ok && wait(&sh->p_full[i][0], p_phase[i], 86);
+          ok = ok && wait(&sh->p_full[i][0], (p_phases >> i) & 1, 86);
           if (!ok) break;
           tc_fence_after();
-          outputs(i, 0, r_lo + (uint32_t)v_stage * (kTileBytes >> 4), t > w.t0);
-          if (elected) umma_commit(smem_u32(&sh->half_done[i]));
-          ok = wait(&sh->p_full[i][1], p_phase[i], 79);
-          p_phase[i] ^= 1;
+          if (elected) {
+            outputs(i, 0, v_lo, t > w.t0);
+            umma_commit(smem_u32(&sh->half_done[i]));
+          }
+          ok = wait(&sh->p_full[i][1], (p_phases >> i) & 1, 79);
+          p_phases ^= 1u << i;
           if (!ok) break;
           tc_fence_after();
-          outputs(i, 1, r_lo + (uint32_t)v_stage * (kTileBytes >> 4), true);
-          if (i == tiles - 1 && elected) umma_commit(smem_u32(&sh->empty[v_stage]));
-          if (more_keys) {
-            if (i == 0) {
-              ok = wait(&sh->full[k_stage], phase, 87);
-              if (!ok) break;
-              tc_fence_after();
+          if (elected) {
+            outputs(i, 1, v_lo, true);
+            if (i == tiles - 1) umma_commit(smem_u32(&sh->empty[v_stage]));
+            if (more_keys) {
+              scores(i, k_lo);
+              if (i == tiles - 1) {
+                umma_commit(smem_u32(&sh->empty[k_stage]));
+                if (t + 2 == w.t1) umma_commit(smem_u32(&sh->q_empty));
+              }
+            } else {
+              umma_commit(smem_u32(&sh->o_full[i]));
             }
-            scores(i, r_lo + (uint32_t)k_stage * (kTileBytes >> 4));
-            if (i == tiles - 1 && elected) {
-              umma_commit(smem_u32(&sh->empty[k_stage]));
-              if (t + 2 == w.t1) umma_commit(smem_u32(&sh->q_empty));
-            }
-          } else if (elected) {
-            umma_commit(smem_u32(&sh->o_full[i]));
           }
         }
         if (more_keys) next_stage();
