@@ -216,7 +216,7 @@ cudaError_t launch_attend(const Launch& L, const CacheSeqs& cs, const CacheGeom&
     *drv_err = (int)encode_queries(encode, cs, g, q, p.tc.as.tile_tokens, &q_map);
     if (*drv_err != 0) return cudaErrorUnknown;
     const AttendWs w = attend_ws(ws, p.tc.grid, p.tc.as.rows);
-    e = launch_attend_tc(L, g, p.tc.as, w, p.tc.grid, o, q_map, k_map, v_map);
+    e = launch_attend_tc(L, g, p.tc.as, w, p.tc.grid, o, v, q_map, k_map, v_map);
     if (e == cudaSuccess) e = launch_attend_join(L, g, p.tc.as, w, p.tc.grid, o);
   }
   if (e == cudaSuccess && p.rows.as.num > 0) {

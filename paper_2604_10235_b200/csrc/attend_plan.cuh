@@ -203,6 +203,16 @@ struct AttendWalk {
   __device__ __forceinline__ int slot() const { return 2 * (int)blockIdx.x + (t0 == 0 ? 1 : 0); }
 };
 
+// Pairs of bf16: a mask of the finite ones, and whether any of eight is infinite or no number.
+__device__ __forceinline__ uint32_t odd_halves(uint32_t two) { return ((two & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
+__device__ __forceinline__ uint32_t finite_halves(uint32_t two) {
+  const uint32_t odd = odd_halves(two);
+  return (odd & 0x8000u ? 0u : 0xffffu) | (odd & 0x80000000u ? 0u : 0xffff0000u);
+}
+__device__ __forceinline__ bool any_odd(const uint4& x) {
+  return (odd_halves(x.x) | odd_halves(x.y) | odd_halves(x.z) | odd_halves(x.w)) != 0;
+}
+
 // Workspace of a launch: per CTA the place at which its share begins, then two partial results per CTA: outputs
 // [rows][128], then (maximum in units of log2, sum) [rows].
 struct AttendWs {
@@ -233,7 +243,7 @@ cudaError_t launch_attend_join(const Launch& L, const CacheGeom& g, const Attend
 cudaError_t launch_attend_rows(const Launch& L, const CacheGeom& g, const AttendSeqs& as, const AttendWs& ws,
                                int grid, const AttendOut& o, const void* q, const CUtensorMap& k_map, const CUtensorMap& v_map);
 cudaError_t launch_attend_tc(const Launch& L, const CacheGeom& g, const AttendSeqs& as, const AttendWs& ws,
-                             int grid, const AttendOut& o, const CUtensorMap& q_map, const CUtensorMap& k_map,
+                             int grid, const AttendOut& o, const void* v, const CUtensorMap& q_map, const CUtensorMap& k_map,
                              const CUtensorMap& v_map);
 constexpr int kTcTile = 128;         // keys per tile of attend_tc.cu, and query rows per tile (two tiles a block)
 constexpr int kRowsTile = 64;        // keys per tile of attend_rows.cu

@@ -217,6 +217,9 @@ attend_rows_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
                                         tile_at(quarter * 16 + (i >> 4), i & 15)) = make_uint4(0u, 0u, 0u, 0u);
             __syncwarp();
           }
+          // Of the keys that some of the rows attend to and others do not, values of V that are infinite or no numbers would
+          // reach them all (0 x inf): they count for the rows that attend to them here, and the product finds zeros.
+          const bool shared_edge = edge && least < most;
           float x[2][4];                 // [row][key]: keys key0 + 2 (lane % 4) + {0, 1, 8, 9}
           float top[2];
 #pragma unroll
@@ -244,6 +247,30 @@ attend_rows_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
               }
             }
           }
+          if (shared_edge) {
+            uint8_t* v_rows = ring + (size_t)stage * 2 * kTileBytes + kTileBytes;
+            bool odd = false;
+            for (int i = lane; i < 16 * 16; i += 32) odd |= any_odd(*reinterpret_cast<const uint4*>(v_rows + tile_at(quarter * 16 + (i >> 4), i & 15)));
+            if (__any_sync(0xffffffffu, odd)) {
+              for (int key = 0; key < 16; ++key) {
+#pragma unroll
+                for (int c = 0; c < 16; ++c) {
+                  uint32_t* at = reinterpret_cast<uint32_t*>(v_rows + tile_at(quarter * 16 + key, c) + 4 * (lane & 3));
+                  const uint32_t both = *at, keep = finite_halves(both);
+                  const float bad[2] = {__uint_as_float((both & ~keep) << 16), __uint_as_float((both & ~keep) & 0xffff0000u)};
+#pragma unroll
+                  for (int i = 0; i < 2; ++i)
+                    if (key0 + key < lim[i]) {
+                      acc[c][2 * i] += bad[0];
+                      acc[c][2 * i + 1] += bad[1];
+                    }
+                  __syncwarp();
+                  *at = both & keep;
+                }
+              }
+              __syncwarp();
+            }
+          }
           uint32_t pa[4];
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
@@ -262,7 +289,7 @@ attend_rows_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
             mma16816(acc[c], pa, vb[0], vb[1]);
             mma16816(acc[c + 1], pa, vb[2], vb[3]);
           }
-          if (key0 + 16 > most) fence_proxy_async();        // this warp's stores before the copy that comes next
+          if (edge) fence_proxy_async();                   // this warp's stores before the copy that comes next
         }
         __syncwarp();
         if (lane == 0) mbar_arrive(smem_u32(&sh->empty[stage]));

@@ -45,6 +45,7 @@ struct Shared {
   uint64_t s_full[2], p_full[2][2], half_done[2], o_full[2], o_empty[2];       // per tile of the block (P: per half of it)
   uint32_t tmem_base;
   int abort_flag;
+  int odd_values;                // V has had infinities or no numbers among keys that only some rows of a block attend to
 };
 constexpr size_t kSmem = 1024 + (size_t)(kStages + 2) * kTileBytes + sizeof(Shared);
 static_assert(kSmem <= kSmemPerCta, "shared memory of a CTA");
@@ -135,7 +136,7 @@ __device__ __forceinline__ void hand_over(uint32_t bar, int lane) {
 __global__ void __launch_bounds__(kThreads, 1)
 attend_tc_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
                  const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
-                 const __grid_constant__ CUtensorMap v_map, const AttendOut o, const AttendWs ws, DeviceStatus* status) {
+                 const __grid_constant__ CUtensorMap v_map, const uint16_t* __restrict__ v_pool, const AttendOut o, const AttendWs ws, DeviceStatus* status) {
   extern __shared__ uint8_t dyn[];
   uint8_t* q_smem = dyn + ((1024u - (smem_u32(dyn) & 1023u)) & 1023u);
   uint8_t* ring = q_smem + 2 * kTileBytes;
@@ -164,6 +165,7 @@ attend_tc_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
       mbar_init(smem_u32(&sh->q_full), 1);
       mbar_init(smem_u32(&sh->q_empty), 1);
       sh->abort_flag = 0;
+      sh->odd_values = 0;
     }
     fence_barrier_init();
     __syncwarp();
@@ -338,6 +340,7 @@ attend_tc_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
       const int lim = real ? (g.causal ? max(0, w.q.n - w.q.T + tok + 1) : w.q.n) : 0;     // keys that the row attends to
       const bool idle = !__any_sync(0xffffffffu, real);
       const int least = __reduce_min_sync(0xffffffffu, real ? lim : 0x7fffffff);
+      const int shared = g.causal ? max(0, w.q.n - w.q.T + w.at.b * as.block_tokens + 1) : w.q.n;       // keys from here on: not by all rows
       const int plain = min(least, w.limit) / kTcTile;         // tiles before this one have no masked keys
       float ref = -INFINITY;
       uint64_t sum[2] = {0ull, 0ull};
@@ -345,13 +348,29 @@ attend_tc_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
         if (!dead) dead = !wait(&sh->s_full[i], s_phase, 88 + i);
         s_phase ^= 1;
         const int key0 = t * kTcTile;
-        if (t >= plain && !dead && i == 0 && key0 + kTcTile > w.limit) {
-          // rows of V that no row of the block attends to may hold anything: 0 x NaN.  (Both products with V wait for this tile's P.)
+        if (i == 0 && key0 + kTcTile > shared && !dead) {
+          // Rows of V that no row of the block attends to may hold anything, and infinities of rows that only some attend to
+          // would reach all (0 x inf): the products find zeros, and the latter count at the end.  (Both products with V come behind this
+          // tile's P.)
           const int stage = entry % kStages;
           dead = !wait(&sh->full[stage], (entry / kStages) & 1, 90);
-          for (int e = (w.limit - key0) * 16 + (int)threadIdx.x; e < kTcTile * 16; e += 128)
-            *reinterpret_cast<uint4*>(ring + (size_t)stage * kTileBytes + (e >> 7) * 2048 + ((e >> 3) & 1) * 1024 +
-                                      ((e >> 4) & 7) * 128 + (e & 7) * 16) = make_uint4(0u, 0u, 0u, 0u);
+          for (int e = max(0, shared - key0) * 16 + (int)threadIdx.x; e < kTcTile * 16; e += 128) {
+            uint4* at = reinterpret_cast<uint4*>(ring + (size_t)stage * kTileBytes + (e >> 7) * 2048 + ((e >> 3) & 1) * 1024 +
+                                                 ((e >> 4) & 7) * 128 + (e & 7) * 16);
+            if (key0 + (e >> 4) >= w.limit) {
+              *at = make_uint4(0u, 0u, 0u, 0u);
+            } else {
+              uint4 x = *at;
+              if (any_odd(x)) {
+                x.x &= finite_halves(x.x);
+                x.y &= finite_halves(x.y);
+                x.z &= finite_halves(x.z);
+                x.w &= finite_halves(x.w);
+                *at = x;
+                sh->odd_values = 1;
+              }
+            }
+          }
           fence_proxy_async();
         }
         if (!dead) tc_fence_after();
@@ -461,6 +480,22 @@ attend_tc_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
 #pragma unroll
             for (int e = 0; e < 32; ++e) x[e] = 0u;
           }
+          if (real && *(volatile int*)&sh->odd_values) {
+            const int32_t* table = g.table + (int64_t)as.src[w.at.i] * g.table_stride;
+#pragma unroll 1
+            for (int key = max(shared, w.t0 * kTcTile); key < min(lim, w.t1 * kTcTile); ++key) {
+              const int page = table[key >> g.page_shift];
+              if (page < 0 || page >= g.pool_pages) continue;
+              const uint32_t* v_row = reinterpret_cast<const uint32_t*>(
+                  v_pool + (((int64_t)page << g.page_shift) + (key & ((1 << g.page_shift) - 1))) * g.kv_tok + (int64_t)w.at.h * g.kv_head) + c * 16;
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                const uint32_t two = v_row[e], bad = two & ~finite_halves(two);
+                x[2 * e] = __float_as_uint(__uint_as_float(x[2 * e]) + __uint_as_float(bad << 16));
+                x[2 * e + 1] = __float_as_uint(__uint_as_float(x[2 * e + 1]) + __uint_as_float(bad & 0xffff0000u));
+              }
+            }
+          }
           if (real && whole) {
             uint4* dst = reinterpret_cast<uint4*>(o.out + row * g.out_tok + h * g.out_head + c * 32);
 #pragma unroll
@@ -503,12 +538,12 @@ attend_tc_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
 }  // namespace
 
 cudaError_t launch_attend_tc(const Launch& L, const CacheGeom& g, const AttendSeqs& as, const AttendWs& ws,
-                             int grid, const AttendOut& o, const CUtensorMap& q_map, const CUtensorMap& k_map,
+                             int grid, const AttendOut& o, const void* v, const CUtensorMap& q_map, const CUtensorMap& k_map,
                              const CUtensorMap& v_map) {
   const cudaError_t e = allow_smem(attend_tc_kernel);
   if (e != cudaSuccess) return e;
   return launch_pdl(attend_tc_kernel, dim3((unsigned)grid), dim3(kThreads), kSmem, L.stream, 1, g, as, q_map, k_map, v_map,
-                    o, ws, L.status);
+                    (const uint16_t*)v, o, ws, L.status);
 }
 
 }  // namespace cc

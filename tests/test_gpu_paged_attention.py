@@ -227,3 +227,36 @@ def test_not_a_number_where_it_is_attended_to_and_only_there(new):
     assert out[new:, 4:, 9].isinf().all() and torch.isfinite(out[new:, :4]).all()
     rest = [c for c in range(D) if c != 9]
     assert torch.isfinite(out[new:, 4:][..., rest]).all() and torch.isfinite(lse[new:]).all()
+
+
+@pytest.mark.parametrize("heads,new,n", [((8, 2), 4, 70), ((8, 2), 3, 64), ((28, 4), 2, 129), ((8, 2), 40, 300), ((28, 4), 33, 1000),
+                                         ((4, 4), 300, 700), ((16, 1), 70, 70)])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_later_tokens_of_a_chunk_do_not_reach_earlier_ones(heads, new, n, bad):
+    """Infinities and NaN in K and V of a token are seen by the tokens that attend to it only."""
+    hq, hkv = heads
+    cache = Cache([n, n + 5], hkv, 16, seed=n)
+    for token in (new - 1, new // 2):
+        clean_k, clean_v = cache.k.clone(), cache.v.clone()
+        row = cache.rows(0)[n - new + token]
+        cache.v[row, 0, 3] = bad
+        cache.v[row, 0, 77] = bad
+        cache.k[cache.rows(1)[n + 5 - new + token], hkv - 1, 9] = math.nan
+        q, out, lse = attend(ctx(), cache, hq, [new, new])
+        assert ctx().poll() == 0
+        cache.k.copy_(clean_k)
+        cache.v.copy_(clean_v)
+        ref = attend_reference(cache, q, [new, new])
+        g = hq // hkv
+        hit = torch.zeros(out.shape, dtype=torch.bool, device="cuda")
+        hit[token:new, :g, 3] = hit[token:new, :g, 77] = True
+        if math.isnan(bad):
+            assert out[hit].isnan().all()
+        else:
+            assert (out[hit] == bad).all()
+        hit[new + token:, hq - g:] = True
+        assert out[new + token:, hq - g:].isnan().all() and lse[new + token:, hq - g:].isnan().all()
+        out, lse = out.clone(), lse.clone()
+        out[hit] = ref[0].bfloat16()[hit]
+        lse[new + token:, hq - g:] = ref[1].float()[new + token:, hq - g:]
+        assert_attention(out, lse, ref)
