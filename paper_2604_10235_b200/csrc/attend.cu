@@ -1,6 +1,8 @@
 // Attention over a paged cache: which kernel takes which sequences, the tensor maps, the join of cut problems.
 #include <cuda_bf16.h>
 
+#include <stdint.h>
+
 #include <algorithm>
 
 #include "attend_plan.cuh"
@@ -12,17 +14,21 @@ namespace cc {
 namespace {
 
 constexpr int kJoinWarps = 8;
-constexpr int kJoinRows = 8;             // blocks per boundary at most
 
-// Joins the parts of the problems that are cut: blocks per (boundary between two shares, rows), idle unless the boundary is the first
-// inside its problem.  A warp takes a row at a time; the parts follow each other in the order of the CTAs.
+// The join of the problems that are cut: blocks per (boundary between two shares, rows), idle unless the boundary is the first inside
+// its problem.  The parts of a problem follow each other in the order of the CTAs.
 //   out = sum_k 2^(m_k - M) o_k / sum_k 2^(m_k - M) l_k
-// Bound by latency (what it reads is in L2): the places of 31 shares in one load, and the first outputs of a row are asked for
-// together with its statistics.
+// Bound by latency (what it reads is in L2).  FEW rows of many parts (the kernel for few rows): a warp takes a row, and its first eight
+// outputs are asked for together with their statistics.  Many rows of a few parts: eight lanes take a row, all of them two
+// parts at once, so that a warp does four rows in the time of one (a warp per row and four rows after one another: 15 us of
+// the 90 of 517 tokens over 8709 keys).
+template <bool FEW>
 __global__ void __launch_bounds__(kJoinWarps * 32)
-attend_join_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
-                   const AttendWs ws, int grid, const AttendOut o, DeviceStatus* status) {
-  constexpr int kAhead = 8;
+attend_join_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as, const AttendWs ws, int grid, const AttendOut o,
+                   DeviceStatus* status) {
+  constexpr int kLanes = FEW ? 32 : 8;             // per row
+  constexpr int kVecs = 32 / kLanes;               // 16-byte vectors of a row's output per lane
+  constexpr int kAhead = FEW ? 8 : 2;              // parts under way at once
   pdl_launch_dependents();
   pdl_wait();
   const int lane = threadIdx.x & 31;
@@ -46,56 +52,72 @@ attend_join_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
       if (in != 0xffffffffu) break;
     }
   }
-  const int T = as.seq[p.i].T, n = attend_len(as, g, p.i, status);
-  for (int r = blockIdx.y * kJoinWarps + (threadIdx.x >> 5); r < as.rows; r += gridDim.y * kJoinWarps) {
+  const AttendSeq q = as.seq[p.i];
+  const int n = attend_len(as, g, p.i, status);
+  const int l = lane % kLanes;                     // of the row
+  for (int r0 = (blockIdx.y * kJoinWarps + (threadIdx.x >> 5)) * (32 / kLanes); r0 < as.rows; r0 += gridDim.y * kJoinWarps * (32 / kLanes)) {
+    const int r = r0 + lane / kLanes;
     const int in_tile = (r & 127) / g.group, t = p.b * as.block_tokens + (r >> 7) * as.tile_tokens + in_tile;
-    if (in_tile >= as.tile_tokens || t >= T) continue;
+    const bool real = in_tile < as.tile_tokens && t < q.T;
+    if (!__any_sync(0xffffffffu, real)) continue;
     // part 0 is the end of share b - 1, part k the beginning of share b - 1 + k
-    auto entry = [&](int k) { return (int64_t)(k == 0 ? 2 * (b - 1) + 1 : 2 * (b - 1 + k)) * as.rows + r; };
-    auto output = [&](int k) { return __ldcg(reinterpret_cast<const float4*>(ws.out + entry(k) * kHeadDim) + lane); };
-    float4 x[kAhead];
+    auto entry = [&](int k) { return (int64_t)((k == 0 ? 2 * (b - 1) + 1 : 2 * (b - 1 + k)) * as.rows + r); };
+    auto output = [&](int k, int v) { return __ldcg(reinterpret_cast<const float4*>(ws.out + entry(k) * kHeadDim) + v * kLanes + l); };
+    auto stat = [&](int k) { return real && k < parts ? __ldcg(ws.stat + entry(k)) : make_float2(-INFINITY, 0.f); };
+    float4 x[kAhead][kVecs];
+    auto load = [&](int k0) {
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) x[k] = k < parts ? output(k) : make_float4(0.f, 0.f, 0.f, 0.f);
-    const float2 first = lane < parts ? __ldcg(ws.stat + entry(lane)) : make_float2(-INFINITY, 0.f);
-    float top = first.x;
-    for (int k = 32 + lane; k < parts; k += 32) top = fmaxf(top, __ldcg(ws.stat + entry(k)).x);
+      for (int k = 0; k < kAhead; ++k)
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-    float total = 0.f;
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    auto add = [&](float w, const float4& y) {
-      v.x = fmaf(w, y.x, v.x);
-      v.y = fmaf(w, y.y, v.y);
-      v.z = fmaf(w, y.z, v.z);
-      v.w = fmaf(w, y.w, v.w);
+        for (int v = 0; v < kVecs; ++v) x[k][v] = real && k0 + k < parts ? output(k0 + k, v) : make_float4(0.f, 0.f, 0.f, 0.f);
     };
-    for (int k0 = 0; k0 < parts; k0 += 32) {
-      const float2 st = k0 == 0 ? first : k0 + lane < parts ? __ldcg(ws.stat + entry(k0 + lane)) : make_float2(-INFINITY, 0.f);
-      const float f = st.x == -INFINITY ? 0.f : ex2(st.x - top);
-      total += f * st.y;
-      const int m = min(32, parts - k0);
-      if (k0 == 0) {
+    load(0);
+    const float2 first = stat(l);
+    float top = first.x;
+    for (int k = kLanes + l; k < parts; k += kLanes) top = fmaxf(top, stat(k).x);
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-          const float w = __shfl_sync(0xffffffffu, f, k);
-          if (k < m) add(w, x[k]);
+    for (int d = kLanes / 2; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+    float total = 0.f;
+    float4 sum[kVecs];
+#pragma unroll
+    for (int v = 0; v < kVecs; ++v) sum[v] = make_float4(0.f, 0.f, 0.f, 0.f);
+    float f = 0.f;                                 // weight of part k0 + l of every kLanes parts
+    for (int k0 = 0; k0 < parts; k0 += kAhead) {
+      if (k0 > 0) load(k0);
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) {
+        if (k0 + k >= parts) break;
+        if ((k0 + k) % kLanes == 0) {
+          const float2 st = k0 + k == 0 ? first : stat(k0 + k + l);
+          f = st.x == -INFINITY ? 0.f : ex2(st.x - top);
+          total += f * st.y;
+        }
+        const float w = __shfl_sync(0xffffffffu, f, (k0 + k) % kLanes, kLanes);
+#pragma unroll
+        for (int v = 0; v < kVecs; ++v) {
+          sum[v].x = fmaf(w, x[k][v].x, sum[v].x);
+          sum[v].y = fmaf(w, x[k][v].y, sum[v].y);
+          sum[v].z = fmaf(w, x[k][v].z, sum[v].z);
+          sum[v].w = fmaf(w, x[k][v].w, sum[v].w);
         }
       }
-#pragma unroll 8
-      for (int k = k0 == 0 ? kAhead : 0; k < m; ++k) add(__shfl_sync(0xffffffffu, f, k), output(k0 + k));
     }
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
-    const bool none = (g.causal ? n - T + t + 1 : n) <= 0;
+    for (int d = kLanes / 2; d > 0; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
+    if (!real) continue;
+    const bool none = (g.causal ? n - q.T + t + 1 : n) <= 0;
     const float inv = none ? 0.f : 1.0f / total;
-    const int64_t tok = as.seq[p.i].row0 + t;
+    const int64_t tok = q.row0 + t;
     const int h = p.h * g.group + (r & 127) - in_tile * g.group;
-    const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x * inv, v.y * inv), hi = __floats2bfloat162_rn(v.z * inv, v.w * inv);
-    uint2 bits;
-    bits.x = *reinterpret_cast<const uint32_t*>(&lo);
-    bits.y = *reinterpret_cast<const uint32_t*>(&hi);
-    *reinterpret_cast<uint2*>(o.out + tok * g.out_tok + h * g.out_head + lane * 4) = bits;
-    if (o.lse && lane == 0) o.lse[tok * g.hq + h] = none ? -INFINITY : (top + log2f(total)) * 0.6931471805599453f;
+#pragma unroll
+    for (int v = 0; v < kVecs; ++v) {
+      const __nv_bfloat162 lo = __floats2bfloat162_rn(sum[v].x * inv, sum[v].y * inv), hi = __floats2bfloat162_rn(sum[v].z * inv, sum[v].w * inv);
+      uint2 bits;
+      bits.x = *reinterpret_cast<const uint32_t*>(&lo);
+      bits.y = *reinterpret_cast<const uint32_t*>(&hi);
+      *reinterpret_cast<uint2*>(o.out + tok * g.out_tok + h * g.out_head + (v * kLanes + l) * 4) = bits;
+    }
+    if (o.lse && l == 0) o.lse[tok * g.hq + h] = none ? -INFINITY : (top + log2f(total)) * 0.6931471805599453f;
   }
 }
 
@@ -105,6 +127,7 @@ struct AttendPlan {
   AttendSeqs as;
   int grid;
 };
+constexpr int kSplit = 4;
 constexpr int64_t kFewKeys = 400000;      // (keys x KV heads)
 struct AttendPlans {
   AttendPlan rows, tc;
@@ -152,6 +175,22 @@ AttendPlans plan_attend(const CacheSeqs& cs, const CacheGeom& g, int sm_count) {
     total *= g.hkv;
     if (total >> 31) p.too_much = true;
     x->grid = (int)std::min<int64_t>(total, sm_count);
+    // Fewer problems than SMs, and all alike: as many CTAs for each.  A CTA then has part of one problem instead of the end of one and
+    // the beginning of another, which costs it a start and an end (kSplit tiles; 517 tokens over 8709 keys 96 -> 90 us).
+    int64_t problems = 0, most = 0, least = INT64_MAX;
+    for (int i = 0; i < as.num; ++i) {
+      const int64_t n = as.seq[i].n, first = g.causal ? std::max<int64_t>(0, n - as.seq[i].T) : n;
+      problems += (int64_t)as.seq[i].blocks * g.hkv;
+      most = std::max(most, (n + (1 << as.tile_shift) - 1) >> as.tile_shift);
+      least = std::min(least, first >> as.tile_shift);
+    }
+    if (x == &p.tc && problems > 0 && problems <= x->grid) {
+      const int64_t each = x->grid / problems;
+      if (least >= 2 * each && most / each < total / x->grid + kSplit) {
+        x->as.each = (int)each;
+        x->grid = (int)(each * problems);
+      }
+    }
   }
   return p;
 }
@@ -185,9 +224,11 @@ CUresult encode_queries(EncodeTiledFn encode, const CacheSeqs& cs, const CacheGe
 cudaError_t launch_attend_join(const Launch& L, const CacheGeom& g, const AttendSeqs& as, const AttendWs& ws,
                                int grid, const AttendOut& o) {
   if (grid < 2) return cudaSuccess;
-  const int y = std::min((as.rows + kJoinWarps - 1) / kJoinWarps, kJoinRows);
-  return launch_pdl(attend_join_kernel, dim3((unsigned)(grid - 1), (unsigned)y),
-                    dim3(kJoinWarps * 32), 0, L.stream, 1, g, as, ws, grid, o, L.status);
+  const bool few = as.rows <= kRowsMost;
+  const int rows = kJoinWarps * (few ? 1 : 4);     // of a block at a time
+  auto kern = few ? attend_join_kernel<true> : attend_join_kernel<false>;
+  return launch_pdl(kern, dim3((unsigned)(grid - 1), (unsigned)((as.rows + rows - 1) / rows)), dim3(kJoinWarps * 32), 0, L.stream, 1, g,
+                    as, ws, grid, o, L.status);
 }
 
 size_t attend_ws_bytes(const CacheSeqs& cs, const CacheGeom& g, int sm_count) {

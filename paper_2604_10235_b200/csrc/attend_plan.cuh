@@ -25,6 +25,7 @@ struct AttendSeqs {            // the sequences of one launch
   int tile_shift;              // keys per tile = 1 << tile_shift
   int start_weight;            // weight of a problem's start, in tiles (at least 1)
   int rows;                    // rows of a block (and of a partial result)
+  int each;                    // > 0: no shares by weight, every problem has that many CTAs
   AttendSeq seq[CC_MAX_SEQS];
   uint8_t src[CC_MAX_SEQS];    // index of the sequence in the call
 };
@@ -65,7 +66,8 @@ __device__ __forceinline__ void attend_weigh(const CacheGeom& g, const AttendSeq
     q.n = attend_len(as, g, i, st);
     sh->seq[i] = q;
     // (of a causal chunk of several blocks each block has a limit of its own: below)
-    if (q.blocks == 1 || !g.causal) sh->weight[i + 1] = (unsigned)q.blocks * (as.start_weight + attend_tiles(q, as, g.causal, 0));
+    if (as.each) sh->weight[i + 1] = (unsigned)q.blocks;
+    else if (q.blocks == 1 || !g.causal) sh->weight[i + 1] = (unsigned)q.blocks * (as.start_weight + attend_tiles(q, as, g.causal, 0));
     else blocks = true;
   }
   if (__syncthreads_or(blocks)) {
@@ -97,7 +99,7 @@ __device__ __forceinline__ void attend_weigh(const CacheGeom& g, const AttendSeq
 
 // CTAs that get a share.
 __device__ __forceinline__ int attend_workers(const AttendSeqs& as, const AttendShare* sh, int hkv, int grid) {
-  return (int)min(sh->weight[as.num] * (unsigned)hkv, (unsigned)grid);
+  return (int)min(sh->weight[as.num] * (unsigned)hkv * max(as.each, 1), (unsigned)grid);
 }
 
 // The place at which the share of CTA `cta` of `workers` begins (cta == workers: behind everything); one whole warp.
@@ -107,7 +109,8 @@ __device__ __forceinline__ Place attend_place(const CacheGeom& g, const AttendSe
   Place p = {g.hkv, 0, 0, 0};
   if (cta >= workers) return p;
   const unsigned each = total / (unsigned)workers, extra = total - each * (unsigned)workers;
-  const unsigned at = each * (unsigned)cta + extra * (unsigned)cta / (unsigned)workers;          // floor(total * cta / workers)
+  const unsigned at = as.each ? (unsigned)(cta / as.each)
+                              : each * (unsigned)cta + extra * (unsigned)cta / (unsigned)workers;    // floor(total * cta / workers)
   p.h = (int)(at / per_head);
   unsigned rest = at - per_head * (unsigned)p.h;
   const int e0 = 2 * lane, e1 = 2 * lane + 1;
@@ -117,6 +120,22 @@ __device__ __forceinline__ Place attend_place(const CacheGeom& g, const AttendSe
   p.i = m0 ? 2 * (__ffs(m0) - 1) : 2 * (__ffs(m1) - 1) + 1;
   rest -= sh->weight[p.i];
   const AttendSeq q = sh->seq[p.i];
+  if (as.each) {
+    p.b = (int)rest;
+    const int tiles = attend_tiles(q, as, g.causal, p.b), part = cta % as.each;
+    p.tile = part * ((tiles + as.each - 1) / as.each);
+    if (part > 0 && p.tile >= tiles) {             // (fewer tiles than CTAs: the next problem's beginning)
+      p.tile = 0;
+      if (++p.b == q.blocks) {
+        p.b = 0;
+        if (++p.i == as.num) {
+          p.i = 0;
+          ++p.h;
+        }
+      }
+    }
+    return p;
+  }
   if (q.blocks == 1) {
     p.tile = max(0, (int)rest - as.start_weight);
     return p;
