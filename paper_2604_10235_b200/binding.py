@@ -185,6 +185,7 @@ class Context:
         if rc != CC_OK:
             raise CodecompError(rc, self.lib.cc_status_string(rc).decode())
         self.handle = h
+        self._raw = h.value             # for the calls on a cache, whose host time counts
 
     def call(self, name: str, desc: "Desc", *args) -> None:
         """Calls entry point ``name`` with this context, the descriptor and the arguments."""
@@ -192,10 +193,17 @@ class Context:
         if rc:
             self.check(rc)
 
+    def call_cache(self, name: str, desc: "CacheDesc", *args) -> None:
+        """Calls an entry point that works on a cache."""
+        rc = self.lib.calls[name](self._raw, desc.address, self.device, *args)
+        if rc:
+            self.check(rc)
+
     def close(self) -> None:
         if getattr(self, "handle", None):
             self.lib.cc_destroy(self.handle)
             self.handle = None
+            self._raw = 0
 
     def __del__(self):
         try:
@@ -373,6 +381,7 @@ class CacheDesc:
             c.rope_dims, c.rope_interleaved, c.rope_scale = rope.dims, 1 if rope.interleaved else 0, rope.attn_factor
             c.rope_freqs = rope.freqs.ctypes.data_as(C.POINTER(C.c_uint64))
         self.c = c
+        self.address = C.addressof(c)
 
     @property
     def lens(self):
@@ -401,9 +410,7 @@ def _raw_on(ctx: "Context", stream: Optional[int]) -> int:
     """The stream as an integer; None is torch's current stream of the context's device."""
     if stream is not None:
         return stream
-    if _CURRENT_RAW is None:
-        return torch.cuda.current_stream(ctx.device).cuda_stream
-    return _CURRENT_RAW(ctx.device)
+    return torch.cuda.current_stream(ctx.device).cuda_stream if _CURRENT_RAW is None else _CURRENT_RAW(ctx.device)
 
 
 def _stream(stream: Optional[int]) -> C.c_void_p:
@@ -552,13 +559,13 @@ def cc_workspace_views(ctx: Context, desc: Desc, ws: torch.Tensor):
 
 def cc_rope_append(ctx: Context, desc: CacheDesc, q_new, k_new, v_new, positions, q, k, v, stream=None):
     """Rotates the new tokens' queries into ``q`` and appends rotated keys and values to the cache ``k``, ``v``."""
-    ctx.call("cc_rope_append", desc, ctx.device, q_new, k_new, v_new, positions, q, k, v, _raw_on(ctx, stream))
+    ctx.call_cache("cc_rope_append", desc, q_new, k_new, v_new, positions, q, k, v, _raw_on(ctx, stream))
 
 
 def cc_paged_attention(ctx: Context, desc: CacheDesc, q, k, v, out, lse=None, ws=None, stream=None):
     """Attention of the new tokens over the cache into ``out`` (and ``lse``)."""
     ws = ctx.cache_workspace(desc) if ws is None else ws
-    ctx.call("cc_paged_attention", desc, ctx.device, q, k, v, out, lse, ws, _raw_on(ctx, stream))
+    ctx.call_cache("cc_paged_attention", desc, q, k, v, out, lse, ws, _raw_on(ctx, stream))
 
 
 def cc_fork_pages(ctx: Context, desc: CacheDesc, k_layers, v_layers, parents, child_table, free_pages, stream=None):
@@ -571,5 +578,5 @@ def cc_fork_pages(ctx: Context, desc: CacheDesc, k_layers, v_layers, parents, ch
         raise ValueError("as many value pools as key pools, a fresh page and a row of child_table per child are needed")
     if not child_table.is_contiguous() or not free_pages.is_contiguous():
         raise ValueError("child_table and free_pages must be contiguous")
-    ctx.call("cc_fork_pages", desc, ctx.device, len(k_layers), k_layers, v_layers, parents, children, child_table,
+    ctx.call_cache("cc_fork_pages", desc, len(k_layers), k_layers, v_layers, parents, children, child_table,
              child_table.shape[1], free_pages, _raw_on(ctx, stream))

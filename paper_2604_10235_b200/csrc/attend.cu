@@ -241,7 +241,7 @@ cudaError_t launch_attend(const Launch& L, const CacheSeqs& cs, const CacheGeom&
                           void* out, float* lse, void* ws, void* encode_fn, int* drv_err) {
   *drv_err = 0;
   const EncodeTiledFn encode = (EncodeTiledFn)encode_fn;
-  const AttendOut o = {(uint16_t*)out, lse};
+  const AttendOut o = {(uint16_t*)out, lse, (uintptr_t)out % 32 == 0 && g.out_tok % 16 == 0 && g.out_head % 16 == 0};
   const AttendPlans p = plan_attend(cs, g, L.sm_count);
   if (p.too_much) return cudaErrorInvalidConfiguration;
   CUtensorMap q_map, k_map, v_map;

@@ -253,6 +253,7 @@ inline AttendWs attend_ws(void* ws, int grid, int rows) {
 struct AttendOut {
   uint16_t* out;
   float* lse;                        // or null
+  bool wide;                         // rows of out begin on 32-byte boundaries
 };
 
 // Launches the join of cut problems (attend.cu).

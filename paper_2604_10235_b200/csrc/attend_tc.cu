@@ -11,8 +11,8 @@
 // core works on the other tile, and P goes to it in two halves, so that the product with V starts when the first is there.
 //
 // The reference of a row's exponentials need not be its maximum, only near it: P up to 2^24 rounds to bf16 and sums in f32 like
-// P up to 1.  So only the first tile of a row and masked ones look at their maximum beforehand, the others compute with
-// the reference that there is; where the sum of a half tile shows that a logit is far above it (or no number), nothing has been
+// P up to 1.  So only tiles with masked keys look at their maximum beforehand, the others compute with the reference that there is
+// (of a row's first keys); where the sum of a half tile shows that a logit is far above it (or no number), nothing has been
 // handed over yet, the row's maximum becomes the reference, its O is scaled in tensor memory and the half is computed again.
 // One pair of exponentials in eight is evaluated on the FMA pipe (exp2_poly.cuh): 2048 x 32768 1057 us with one in four, 1054 with one in
 // eight, 1077 with one in sixteen; 517 x 8709 96.3, 94.1, 94.7.
@@ -54,6 +54,10 @@ __device__ __forceinline__ float max3_nan(float a, float b, float c) {
   float d;
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
+}
+__device__ __forceinline__ void store32(void* p, const uint32_t* v) {      // 32 bytes, on a 32-byte boundary
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7]) : "memory");
 }
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   uint32_t r;
@@ -377,15 +381,16 @@ attend_tc_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
         if (!dead && !idle) {
           const uint32_t p_bar = smem_u32(&sh->p_full[i][0]);
           int from = 0;                            // first chunk of 32 keys that is not handed over yet
-          if (t > w.t0 && t < plain) {
-            // With the reference that there is.
+          if (t < plain) {
+            // With the reference that there is, in the first tile the maximum of its first 32 keys.
             uint32_t v0[32], v1[32], p0[16], p1[16];
             float reach = -INFINITY;
             uint64_t part[2] = {0ull, 0ull};
-            const uint64_t off2 = offset_of(ref);
             tmem_ld32(s_addr, v0);
             tmem_ld32(s_addr + 32, v1);
             tmem_wait_ld();
+            if (t == w.t0) ref = max32_nan(v0) * c2;
+            const uint64_t off2 = offset_of(ref);
             exponentials<true>(v0, c22, off2, p0, part, reach);
             exponentials<true>(v1, c22, off2, p1, part, reach);
             if (!out_of_range(real, part, reach, c2, ref)) {
@@ -416,7 +421,7 @@ attend_tc_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
             }
           }
           if (from < 4) {
-            // The maximum first: the first tile of a row, tiles with masked keys, logits far above the reference.
+            // The maximum first: tiles with masked keys, logits far above the reference.
             const int last = t >= plain ? lim - key0 : kTcTile;
             float high = -INFINITY;
             uint32_t v[32];
@@ -497,19 +502,22 @@ attend_tc_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
             }
           }
           if (real && whole) {
-            uint4* dst = reinterpret_cast<uint4*>(o.out + row * g.out_tok + h * g.out_head + c * 32);
+            uint16_t* dst = o.out + row * g.out_tok + h * g.out_head + c * 32;
+            uint32_t y[16];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              uint32_t y[4];
+            for (int e = 0; e < 16; ++e)
+              y[e] = lim <= 0 ? 0u : pack_bf16(__uint_as_float(x[2 * e]) * inv, __uint_as_float(x[2 * e + 1]) * inv);
+            if (o.wide) {
+              store32(dst, y);
+              store32(dst + 16, y + 8);
+            } else {
 #pragma unroll
-              for (int k = 0; k < 4; ++k)
-                y[k] = lim <= 0 ? 0u : pack_bf16(__uint_as_float(x[8 * e + 2 * k]) * inv, __uint_as_float(x[8 * e + 2 * k + 1]) * inv);
-              dst[e] = make_uint4(y[0], y[1], y[2], y[3]);
+              for (int e = 0; e < 4; ++e) reinterpret_cast<uint4*>(dst)[e] = make_uint4(y[4 * e], y[4 * e + 1], y[4 * e + 2], y[4 * e + 3]);
             }
           } else if (real) {
-            uint4* dst = reinterpret_cast<uint4*>(ws.out + at * kHeadDim + c * 32);
+            float* dst = ws.out + at * kHeadDim + c * 32;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) dst[e] = make_uint4(x[4 * e], x[4 * e + 1], x[4 * e + 2], x[4 * e + 3]);
+            for (int e = 0; e < 4; ++e) store32(dst + 8 * e, x + 8 * e);
           }
           __syncwarp();
         }
