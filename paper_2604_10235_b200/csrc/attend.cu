@@ -167,6 +167,10 @@ AttendPlans plan_attend(const CacheSeqs& cs, const CacheGeom& g, int sm_count) {
     as.seq[as.num] = AttendSeq{cs.new_off[s], T, cs.kv_len[s], (T + as.block_tokens - 1) / as.block_tokens};
     as.src[as.num++] = (uint8_t)s;
   }
+  // Rows that a block can have (a short chunk has fewer than two tiles of them).
+  int64_t longest = 0;
+  for (int i = 0; i < many.num; ++i) longest = std::max<int64_t>(longest, many.seq[i].T);
+  if (longest <= many.tile_tokens) many.rows = ((int)longest * g.group + 31) / 32 * 32;
   for (AttendPlan* x : {&p.rows, &p.tc}) {
     const AttendSeqs& as = x->as;
     int64_t total = 0;                             // of the weights (attend_weigh), at the longest
