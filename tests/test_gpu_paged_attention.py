@@ -260,3 +260,75 @@ def test_later_tokens_of_a_chunk_do_not_reach_earlier_ones(heads, new, n, bad):
         out[hit] = ref[0].bfloat16()[hit]
         lse[new + token:, hq - g:] = ref[1].float()[new + token:, hq - g:]
         assert_attention(out, lse, ref)
+
+
+@pytest.mark.parametrize("hq,hkv", [(17, 1), (48, 2), (64, 1), (100, 1), (128, 1), (12, 1)])
+@pytest.mark.parametrize("new,n", [(1, 300), (5, 5), (9, 1000)])
+def test_wide_groups(hq, hkv, new, n):
+    check(Cache([n, n + 1], hkv, 16, seed=hq), hq, [new, 1])
+
+
+@pytest.mark.parametrize("causal", [True, False])
+def test_chunks_over_nothing_and_next_to_nothing(causal):
+    check(Cache([0, 1, 0, 130], 2, 16, seed=1), 8, [40, 70, 1, 50], causal)
+
+
+@pytest.mark.parametrize("page", [8, 128])
+@pytest.mark.parametrize("new", [[30, 1, 200], [513]])
+def test_chunks_on_small_and_large_pages(page, new):
+    check(Cache([700 + 3 * t for t in new], 4, page, seed=page), 28, new)
+
+
+@pytest.mark.parametrize("new", [1, 3, 64, 300])
+@pytest.mark.parametrize("scale", [2.0, 40.0])
+def test_logits_of_hundreds(new, scale):
+    """Probabilities that underflow and references that jump by more than a probability's range from tile to tile."""
+    cache = Cache([1200], 2, 16, seed=31)
+    r = cache.rows(0)
+    cache.k[r[::130]] *= 8
+    check(cache, 8, [new], scale=scale)
+
+
+@pytest.mark.parametrize("new", [1, 5, 90])
+def test_equal_keys_give_the_mean(new):
+    cache = Cache([777], 2, 16, seed=32)
+    r = cache.rows(0)
+    cache.k[r] = cache.k[r[:1]].clone()
+    check(cache, 8, [new])
+
+
+def test_mixed_batches_in_one_and_in_two_launches():
+    """Single tokens beside chunks: together where they have few keys, in launches of their own where they have many."""
+    check(Cache([500, 300, 90, 1000], 8, 16, seed=33), 32, [1, 100, 1, 1])
+    check(Cache([30000, 300, 40000, 1000], 8, 16, seed=34), 32, [1, 100, 1, 1])
+
+
+def test_two_streams_with_a_workspace_each():
+    caches = [Cache([20000, 50], 4, 16, seed=35), Cache([9000], 4, 32, seed=36)]
+    news = [[1, 1], [260]]
+    descs = [c.desc(16, t) for c, t in zip(caches, news)]
+    spaces = [ctx().cache_workspace(d) for d in descs]
+    qs = [torch.randn((sum(t), 16, D), device="cuda").bfloat16() for t in news]
+    outs = [torch.empty_like(q) for q in qs]
+    streams = [torch.cuda.Stream() for _ in news]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for c, d, ws, q, out, st in zip(caches, descs, spaces, qs, outs, streams):
+            with torch.cuda.stream(st):
+                cc.cc_paged_attention(ctx(), d, q, c.k, c.v, out, ws=ws)
+    torch.cuda.synchronize()
+    assert ctx().poll() == 0
+    for c, t, q, out in zip(caches, news, qs, outs):
+        assert_attention(out, None, attend_reference(c, q, t))
+
+
+def test_out_off_the_32_byte_grid():
+    cache = Cache([100], 2, 16, seed=37)
+    for new in (1, 40):
+        q = torch.randn((new, 8, D), device="cuda").bfloat16()
+        big = torch.full((new * 8 * D + 8,), 9.0, dtype=torch.bfloat16, device="cuda")
+        out = big[8:].view(new, 8, D)
+        cc.cc_paged_attention(ctx(), cache.desc(8, [new]), q, cache.k, cache.v, out)
+        assert ctx().poll() == 0
+        assert_attention(out, None, attend_reference(cache, q, [new]))
+        assert (big[:8] == 9.0).all()
