@@ -286,7 +286,8 @@ int cc_select_chunks(cc_ctx* ctx, const float* score, int32_t num_chunks, int32_
  * bound of each, so that a captured graph can be replayed while its sequences grow; a value outside
  * [0, kv_lens[s]] is clamped and flagged.  Work is shared out by the lengths found.
  *
- * These calls run on the context's device, whichever is current. */
+ * These calls run on the context's device, whichever is current.  Calls whose work may overlap on the GPU (streams,
+ * captured graphs) need workspaces of their own. */
 
 #define CC_ROPE_PLAIN  0   /* f_i = base^(-2i / dims) */
 #define CC_ROPE_LINEAR 1   /* f_i / factor: positions divided by the factor */

@@ -7,7 +7,8 @@
 //
 // A warp takes a token, or a part of its heads: eight lanes to a row of 256 bytes, two 16-byte chunks a lane, so that
 // both sides of a pair are in one thread; the lanes of four rows share the work of the sines (two each) and keep all
-// eight in registers for every head of the token.  Bound by HBM: every row is read once and written once.
+// eight in registers for every head of the token.  Bound by HBM: every row is read once and written once (8132 tokens of 32 + 8 + 8
+// heads, 200 MB: 35.1 us, 5.7 TB/s with the launch); few tokens by latency (64 tokens: 2.9 us from a graph).
 #include <cuda_bf16.h>
 
 #include "cache_step.cuh"
