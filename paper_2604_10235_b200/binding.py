@@ -573,10 +573,11 @@ def cc_fork_pages(ctx: Context, desc: CacheDesc, k_layers, v_layers, parents, ch
     ``k_layers`` / ``v_layers``, a copy of the parent's last page in ``free_pages[f]`` where that page is not full."""
     if not isinstance(parents, np.ndarray) or parents.dtype != np.int32:
         parents = np.ascontiguousarray(parents, dtype=np.int32)
-    children = len(parents)
-    if len(k_layers) != len(v_layers) or free_pages.numel() < children or child_table.shape[0] < children:
+    children, layers = len(parents), len(k_layers)
+    rows, width = child_table.shape
+    if layers != len(v_layers) or free_pages.numel() < children or rows < children:
         raise ValueError("as many value pools as key pools, a fresh page and a row of child_table per child are needed")
     if not child_table.is_contiguous() or not free_pages.is_contiguous():
         raise ValueError("child_table and free_pages must be contiguous")
-    ctx.call_cache("cc_fork_pages", desc, len(k_layers), k_layers, v_layers, parents, children, child_table,
-             child_table.shape[1], free_pages, _raw_on(ctx, stream))
+    ctx.call_cache("cc_fork_pages", desc, layers, k_layers, v_layers, parents, children, child_table, width, free_pages,
+                   _raw_on(ctx, stream))

@@ -19,11 +19,12 @@ namespace {
 
 constexpr int kThreads = 128;
 constexpr int kWarps = kThreads / 32;
-// Rows in flight per lane and rows of a warp (a quarter of a token of 32 + 8 + 8 heads), 8 blocks per SM.  8132 tokens of 32 + 8 heads
+// Rows in flight per lane and rows of a warp at most (half a token of 32 + 8 + 8 heads), 8 blocks per SM.  8132 tokens of 32 + 8 heads
 // and 5003 of 28 + 4, us: four in flight, a token per warp, 256 threads (98 registers, 2 blocks) 38.3 and 23.6; 16 rows a warp and two in
-// flight (64 registers) 35.7 and 19.5; with blocks of 128 threads 35.4 and 18.9.
+// flight (64 registers) 35.7 and 19.5; blocks of 128 threads 35.2 and 18.6; 24 rows a warp 35.5 and 17.9, 48 rows 35.1 and 20.7.
+// The first rows asked for before the sines: 38.8 and 18.5.
 constexpr int kUnroll = 2;
-constexpr int kWarpRows = 16;
+constexpr int kWarpRows = 24;
 
 struct RopePtrs {
   const uint16_t *q_new, *k_new, *v_new;
@@ -60,14 +61,13 @@ __device__ __forceinline__ void rotate_pair(uint32_t& a, float c, float s) {
 template <bool INTERLEAVED>
 __global__ void __launch_bounds__(kThreads, 8)
 rope_append_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, const __grid_constant__ RopeFreqs f,
-                   const RopePtrs P, DeviceStatus* status, int parts) {
+                   const RopePtrs P, DeviceStatus* status) {
   __shared__ uint64_t turns[kHeadDim / 2];
   pdl_launch_dependents();
   if (threadIdx.x < kHeadDim / 2) turns[threadIdx.x] = f.turns[threadIdx.x];
   __syncthreads();
   const int lane = threadIdx.x & 31, sub = lane >> 3, l8 = lane & 7;
-  const int64_t item = (int64_t)blockIdx.x * kWarps + (threadIdx.x >> 5);
-  const int tok = (int)(item / parts), part = (int)(item - (int64_t)tok * parts);
+  const int tok = (int)blockIdx.x * kWarps + (threadIdx.x >> 5), part = blockIdx.y, parts = gridDim.y;
   pdl_wait();
   if (tok >= cs.new_off[cs.num_seqs]) return;
 
@@ -172,9 +172,9 @@ cudaError_t launch_rope(const Launch& L, const CacheSeqs& cs, const CacheGeom& g
   // Few tokens: the heads of a token are spread over more warps until every SM has sixteen.
   int parts = (rows + kWarpRows - 1) / kWarpRows;
   while (tokens * parts < (int64_t)L.sm_count * 16 && parts < (rows + 3) / 4) ++parts;
-  const int64_t blocks = (tokens * parts + kWarps - 1) / kWarps;
+  const int64_t blocks = (tokens + kWarps - 1) / kWarps;
   auto kern = f.interleaved ? rope_append_kernel<true> : rope_append_kernel<false>;
-  return launch_pdl(kern, dim3((unsigned)blocks), dim3(kThreads), 0, L.stream, 1, cs, g, f, P, L.status, parts);
+  return launch_pdl(kern, dim3((unsigned)blocks, (unsigned)parts), dim3(kThreads), 0, L.stream, 1, cs, g, f, P, L.status);
 }
 
 }  // namespace cc
