@@ -195,6 +195,8 @@ class Context:
 
     def call_cache(self, name: str, desc: "CacheDesc", *args) -> None:
         """Calls an entry point that works on a cache."""
+        if desc.device != self.device:
+            raise ValueError(f"the page table lies on device {desc.device}, the context is of device {self.device}")
         rc = self.lib.calls[name](self._raw, desc.address, self.device, *args)
         if rc:
             self.check(rc)
@@ -381,7 +383,7 @@ class CacheDesc:
             c.rope_dims, c.rope_interleaved, c.rope_scale = rope.dims, 1 if rope.interleaved else 0, rope.attn_factor
             c.rope_freqs = rope.freqs.ctypes.data_as(C.POINTER(C.c_uint64))
         self.c = c
-        self.address = C.addressof(c)
+        self.address, self.device = C.addressof(c), page_table.get_device()
 
     @property
     def lens(self):
@@ -577,7 +579,5 @@ def cc_fork_pages(ctx: Context, desc: CacheDesc, k_layers, v_layers, parents, ch
     rows, width = child_table.shape
     if layers != len(v_layers) or free_pages.numel() < children or rows < children:
         raise ValueError("as many value pools as key pools, a fresh page and a row of child_table per child are needed")
-    if not child_table.is_contiguous() or not free_pages.is_contiguous():
-        raise ValueError("child_table and free_pages must be contiguous")
     ctx.call_cache("cc_fork_pages", desc, layers, k_layers, v_layers, parents, children, child_table, width, free_pages,
                    _raw_on(ctx, stream))

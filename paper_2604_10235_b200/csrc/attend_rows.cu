@@ -111,8 +111,7 @@ attend_rows_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
     const int copies = kRowsTile / span;
     const uint32_t copy_bytes = (uint32_t)span * kHeadDim * 2;
     const bool elected = elect_one();
-    uint64_t policy;           // K and V of a (sequence, head) with one block of tokens are not read again
-
+    uint64_t policy;           // K and V of a (sequence, head) are read by one block of tokens only
     asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
     int stage = 0, seg = 0;
     uint32_t phase = 0;

@@ -10,7 +10,8 @@
 //   w  a CUDA tensor as two words: address, number of elements
 //   L  a sequence of tensors as a host array of addresses, or None
 //   d  a device number (no word): the tensors of the kinds below are on that device
-//   b, n, f  a CUDA tensor of bfloat16, int32, float32, or None
+//   b        a CUDA tensor of bfloat16, or None
+//   n, f     a contiguous CUDA tensor of int32, float32, or None
 //   M  a sequence of bfloat16 tensors as a host array of addresses
 //   h  a contiguous host array (numpy) of 32-bit integers
 #define PY_SSIZE_T_CLEAN
@@ -29,7 +30,7 @@ namespace {
 
 constexpr int kMaxWords = 20;
 
-PyObject *s_data_ptr, *s_is_cuda, *s_is_pinned, *s_numel, *s_dtype, *s_get_device;
+PyObject *s_data_ptr, *s_is_cuda, *s_is_pinned, *s_numel, *s_dtype, *s_get_device, *s_is_contiguous;
 PyObject *t_bf16, *t_i32, *t_f32;      // torch's types, looked up with the first spec that names one
 
 bool word_of(PyObject* o, uint64_t* out) {
@@ -70,7 +71,7 @@ bool tensor_word(PyObject* o, bool pinned_ok, uint64_t* out) {
 }
 
 // A tensor of the given type on the given device, or None where that is allowed.
-bool typed_word(PyObject* o, PyObject* dtype, long device, bool none_ok, uint64_t* out) {
+bool typed_word(PyObject* o, PyObject* dtype, long device, bool none_ok, bool contiguous, uint64_t* out) {
   if (none_ok && o == Py_None) {
     *out = 0;
     return true;
@@ -83,6 +84,10 @@ bool typed_word(PyObject* o, PyObject* dtype, long device, bool none_ok, uint64_
   if (same && !word_from(o, s_get_device, &at)) return false;
   if (!same || (long)at != device) {
     PyErr_Format(PyExc_ValueError, "libcodecomp takes a tensor of %S on cuda:%ld here", dtype, device);
+    return false;
+  }
+  if (contiguous && !is_true(PyObject_CallMethodNoArgs(o, s_is_contiguous))) {
+    if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "libcodecomp takes a contiguous tensor here");
     return false;
   }
   return word_from(o, s_data_ptr, out);
@@ -159,9 +164,9 @@ PyObject* call_bound(PyObject* self, PyObject* const* args, Py_ssize_t n_args) {
         device = PyLong_AsLong(o);
         ok = !(device == -1 && PyErr_Occurred());
         break;
-      case 'b': ok = typed_word(o, t_bf16, device, true, &a[n++]); break;
-      case 'n': ok = typed_word(o, t_i32, device, true, &a[n++]); break;
-      case 'f': ok = typed_word(o, t_f32, device, true, &a[n++]); break;
+      case 'b': ok = typed_word(o, t_bf16, device, true, false, &a[n++]); break;
+      case 'n': ok = typed_word(o, t_i32, device, true, true, &a[n++]); break;
+      case 'f': ok = typed_word(o, t_f32, device, true, true, &a[n++]); break;
       case 'h': ok = host_word(o, &a[n++]); break;
       case 'M':
       case 'L': {
@@ -173,7 +178,7 @@ PyObject* call_bound(PyObject* self, PyObject* const* args, Py_ssize_t n_args) {
         for (Py_ssize_t j = 0; j < m && ok; ++j) {
           PyObject* item = PySequence_Fast_GET_ITEM(seq, j);
           ok = f->spec[i] == 'L' ? word_from(item, s_data_ptr, &lists.back()[j])
-                                 : typed_word(item, t_bf16, device, false, &lists.back()[j]);
+                                 : typed_word(item, t_bf16, device, false, false, &lists.back()[j]);
         }
         Py_DECREF(seq);
         a[n++] = (uint64_t)(uintptr_t)lists.back().data();
@@ -252,5 +257,6 @@ PyMODINIT_FUNC PyInit__cccall(void) {
   s_numel = PyUnicode_InternFromString("numel");
   s_dtype = PyUnicode_InternFromString("dtype");
   s_get_device = PyUnicode_InternFromString("get_device");
+  s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
   return PyModule_Create(&module);
 }

@@ -207,8 +207,9 @@ def test_typed_arguments_are_checked():
         attend(at, desc, -1, object(), bf, bf, bf, f32, None, 0)
     rope = lib.calls["cc_rope_append"]
     assert rope(at, desc, -1, None, None, None, None, None, None, None, 0) == cc.CC_OK
-    with pytest.raises(ValueError):
-        rope(at, desc, -1, None, None, None, f32, None, None, None, 0)
+    for positions in (f32, torch.zeros((4, 2), dtype=torch.int32)[:, 0]):
+        with pytest.raises(ValueError):
+            rope(at, desc, -1, None, None, None, positions, None, None, None, 0)
     fork = lib.calls["cc_fork_pages"]
     parents = np.array([0, 5], np.int32)
     assert fork(at, desc, -1, 0, [], [], parents, 2, i32, 3, i32, 0) == cc.CC_OK

@@ -215,6 +215,18 @@ def test_bad_pages_are_flagged_and_skipped(new):
     assert_attention(out, lse, attend_reference(cache, q, [new, new]))
 
 
+@pytest.mark.parametrize("new", [1, 50])
+def test_tiles_without_a_good_page(new):
+    cache = Cache([1000, 100], 2, 128, seed=15, poison=False)
+    good = cache.table.clone()
+    cache.table[0] = -1
+    q, out, lse = attend(ctx(), cache, 8, [new, new])
+    assert ctx().poll() == cc.CC_ERR_DEVICE_FLAG
+    cache.table.copy_(good)
+    ref = attend_reference(cache, q, [new, new])
+    assert_attention(out[new:], lse[new:], tuple(x[new:] for x in ref))
+
+
 @pytest.mark.parametrize("new", [1, 20])
 def test_not_a_number_where_it_is_attended_to_and_only_there(new):
     cache = Cache([100, 90], 2, 16, seed=16)
