@@ -18,107 +18,169 @@ constexpr int kJoinWarps = 8;
 // The join of the problems that are cut: blocks per (boundary between two shares, rows), idle unless the boundary is the first inside
 // its problem.  The parts of a problem follow each other in the order of the CTAs.
 //   out = sum_k 2^(m_k - M) o_k / sum_k 2^(m_k - M) l_k
-// Bound by latency (what it reads is in L2).  FEW rows of many parts (the kernel for few rows): a warp takes a row, and its first eight
-// outputs are asked for together with their statistics.  Many rows of a few parts: eight lanes take a row, all of them two
-// parts at once, so that a warp does four rows in the time of one (a warp per row and four rows after one another: 15 us of
-// the 90 of 517 tokens over 8709 keys).
-template <bool FEW>
-__global__ void __launch_bounds__(kJoinWarps * 32)
-attend_join_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as, const AttendWs ws, int grid, const AttendOut o,
-                   DeviceStatus* status) {
-  constexpr int kLanes = FEW ? 32 : 8;             // per row
-  constexpr int kVecs = 32 / kLanes;               // 16-byte vectors of a row's output per lane
-  constexpr int kAhead = FEW ? 8 : 2;              // parts under way at once
-  pdl_launch_dependents();
-  pdl_wait();
+// Bound by latency (what it reads is in L2), so whatever a row needs is asked for at once.
+struct CutProblem {
+  Place p;
+  int first, parts;                                // its first boundary, parts (0: the boundary is not one)
+  // Part 0 is the end of share first - 1, part k the beginning of share first - 1 + k.
+  __device__ __forceinline__ int64_t entry(const AttendSeqs& as, int k, int r) const {
+    return (int64_t)(k == 0 ? 2 * (first - 1) + 1 : 2 * (first - 1 + k)) * as.rows + r;
+  }
+};
+// One whole warp; the places of 31 shares in one load.
+__device__ __forceinline__ CutProblem cut_problem(const CacheGeom& g, const AttendSeqs& as, const AttendWs& ws, int grid, int b) {
   const int lane = threadIdx.x & 31;
-  const int b = blockIdx.x + 1;                    // the share that begins at the boundary
   auto place = [&](int share) {
     const int4 x = share < grid ? __ldcg(reinterpret_cast<const int4*>(ws.place + share)) : make_int4(0, 0, 0, -1);
     return Place{x.x, x.y, x.z, x.w};
   };
   const Place near = place(b - 1 + lane);          // of shares b - 1, b, ...
-  const Place p = {__shfl_sync(0xffffffffu, near.h, 1), __shfl_sync(0xffffffffu, near.i, 1), __shfl_sync(0xffffffffu, near.b, 1),
-                   __shfl_sync(0xffffffffu, near.tile, 1)};
-  auto inside = [&](const Place& x) { return x.tile > 0 && x.h == p.h && x.i == p.i && x.b == p.b; };
+  CutProblem c;
+  c.first = b;
+  c.parts = 0;
+  c.p = Place{__shfl_sync(0xffffffffu, near.h, 1), __shfl_sync(0xffffffffu, near.i, 1), __shfl_sync(0xffffffffu, near.b, 1),
+              __shfl_sync(0xffffffffu, near.tile, 1)};
+  auto inside = [&](const Place& x) { return x.tile > 0 && x.h == c.p.h && x.i == c.p.i && x.b == c.p.b; };
   unsigned in = __ballot_sync(0xffffffffu, inside(near));
-  if (p.tile <= 0 || (in & 1u)) return;
-  if (p.h >= g.hkv || p.i >= as.num || p.b >= as.seq[p.i].blocks) return;      // (another call wrote to this workspace)
-  int parts = __ffs(~(in >> 1));                   // shares b, b + 1, ... that begin inside, and the one before
+  if (c.p.tile <= 0 || (in & 1u)) return c;
+  if (c.p.h >= g.hkv || c.p.i >= as.num || c.p.b >= as.seq[c.p.i].blocks) return c;      // (another call wrote to this workspace)
+  c.parts = __ffs(~(in >> 1));                     // shares b, b + 1, ... that begin inside, and the one before
   if (in == 0xfffffffeu) {
     for (int s0 = b + 31;; s0 += 32) {
       in = __ballot_sync(0xffffffffu, inside(place(s0 + lane)));
-      parts += in == 0xffffffffu ? 32 : __ffs(~in) - 1;
+      c.parts += in == 0xffffffffu ? 32 : __ffs(~in) - 1;
       if (in != 0xffffffffu) break;
     }
   }
-  const AttendSeq q = as.seq[p.i];
-  const int n = attend_len(as, g, p.i, status);
-  const int l = lane % kLanes;                     // of the row
-  for (int r0 = (blockIdx.y * kJoinWarps + (threadIdx.x >> 5)) * (32 / kLanes); r0 < as.rows; r0 += gridDim.y * kJoinWarps * (32 / kLanes)) {
-    const int r = r0 + lane / kLanes;
-    const int in_tile = (r & 127) / g.group, t = p.b * as.block_tokens + (r >> 7) * as.tile_tokens + in_tile;
-    const bool real = in_tile < as.tile_tokens && t < q.T;
-    if (!__any_sync(0xffffffffu, real)) continue;
-    // part 0 is the end of share b - 1, part k the beginning of share b - 1 + k
-    auto entry = [&](int k) { return (int64_t)((k == 0 ? 2 * (b - 1) + 1 : 2 * (b - 1 + k)) * as.rows + r); };
-    auto output = [&](int k, int v) { return __ldcg(reinterpret_cast<const float4*>(ws.out + entry(k) * kHeadDim) + v * kLanes + l); };
-    auto stat = [&](int k) { return real && k < parts ? __ldcg(ws.stat + entry(k)) : make_float2(-INFINITY, 0.f); };
-    float4 x[kAhead][kVecs];
-    auto load = [&](int k0) {
+  return c;
+}
+__device__ __forceinline__ void add_part(float4& v, float w, const float4& x) {
+  v.x = fmaf(w, x.x, v.x);
+  v.y = fmaf(w, x.y, v.y);
+  v.z = fmaf(w, x.z, v.z);
+  v.w = fmaf(w, x.w, v.w);
+}
+// Four channels of a row; lse with the first of them.
+__device__ __forceinline__ void store_row(const CacheGeom& g, const AttendOut& o, int64_t tok, int h, int c, const float4& v, float top,
+                                          float total, bool none) {
+  const float inv = none ? 0.f : 1.0f / total;
+  const __nv_bfloat162 lo = __floats2bfloat162_rn(v.x * inv, v.y * inv), hi = __floats2bfloat162_rn(v.z * inv, v.w * inv);
+  uint2 bits;
+  bits.x = *reinterpret_cast<const uint32_t*>(&lo);
+  bits.y = *reinterpret_cast<const uint32_t*>(&hi);
+  *reinterpret_cast<uint2*>(o.out + tok * g.out_tok + h * g.out_head + c) = bits;
+  if (o.lse && c == 0) o.lse[tok * g.hq + h] = none ? -INFINITY : (top + log2f(total)) * 0.6931471805599453f;
+}
+
+// Few rows of many parts: a block takes a row, each of its warps every eighth part, four of them under way at once.
+__global__ void __launch_bounds__(kJoinWarps * 32)
+attend_join_few_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as, const AttendWs ws, int grid, const AttendOut o,
+                       DeviceStatus* status) {
+  constexpr int kAhead = 4;
+  __shared__ float4 fold[kJoinWarps][32];
+  pdl_launch_dependents();
+  pdl_wait();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = blockIdx.y;
+  const CutProblem c = cut_problem(g, as, ws, grid, blockIdx.x + 1);
+  if (c.parts == 0) return;
+  const AttendSeq q = as.seq[c.p.i];
+  const int in_block = r / g.group, t = c.p.b * as.block_tokens + in_block;
+  if (in_block >= as.block_tokens || t >= q.T) return;
+  auto output = [&](int k) { return __ldcg(reinterpret_cast<const float4*>(ws.out + c.entry(as, k, r) * kHeadDim) + lane); };
+  float4 x[kAhead];
 #pragma unroll
-      for (int k = 0; k < kAhead; ++k)
+  for (int k = 0; k < kAhead; ++k) x[k] = warp + k * kJoinWarps < c.parts ? output(warp + k * kJoinWarps) : make_float4(0.f, 0.f, 0.f, 0.f);
+  auto stat = [&](int k) { return k < c.parts ? __ldcg(ws.stat + c.entry(as, k, r)) : make_float2(-INFINITY, 0.f); };
+  const float2 first = stat(lane);
+  float top = first.x;
+  for (int k = 32 + lane; k < c.parts; k += 32) top = fmaxf(top, stat(k).x);
 #pragma unroll
-        for (int v = 0; v < kVecs; ++v) x[k][v] = real && k0 + k < parts ? output(k0 + k, v) : make_float4(0.f, 0.f, 0.f, 0.f);
-    };
-    load(0);
-    const float2 first = stat(l);
-    float top = first.x;
-    for (int k = kLanes + l; k < parts; k += kLanes) top = fmaxf(top, stat(k).x);
+  for (int d = 16; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+  float total = 0.f;
+  float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int k0 = 0; k0 < c.parts; k0 += 32) {
+    const float2 st = k0 == 0 ? first : stat(k0 + lane);
+    const float f = st.x == -INFINITY ? 0.f : ex2(st.x - top);
+    total += f * st.y;
 #pragma unroll
-    for (int d = kLanes / 2; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
-    float total = 0.f;
-    float4 sum[kVecs];
-#pragma unroll
-    for (int v = 0; v < kVecs; ++v) sum[v] = make_float4(0.f, 0.f, 0.f, 0.f);
-    float f = 0.f;                                 // weight of part k0 + l of every kLanes parts
-    for (int k0 = 0; k0 < parts; k0 += kAhead) {
-      if (k0 > 0) load(k0);
-#pragma unroll
-      for (int k = 0; k < kAhead; ++k) {
-        if (k0 + k >= parts) break;
-        if ((k0 + k) % kLanes == 0) {
-          const float2 st = k0 + k == 0 ? first : stat(k0 + k + l);
-          f = st.x == -INFINITY ? 0.f : ex2(st.x - top);
-          total += f * st.y;
-        }
-        const float w = __shfl_sync(0xffffffffu, f, (k0 + k) % kLanes, kLanes);
-#pragma unroll
-        for (int v = 0; v < kVecs; ++v) {
-          sum[v].x = fmaf(w, x[k][v].x, sum[v].x);
-          sum[v].y = fmaf(w, x[k][v].y, sum[v].y);
-          sum[v].z = fmaf(w, x[k][v].z, sum[v].z);
-          sum[v].w = fmaf(w, x[k][v].w, sum[v].w);
-        }
-      }
+    for (int k = 0; k < kAhead; ++k) {             // (32 parts: four per warp)
+      const int part = warp + k * kJoinWarps;
+      const float w = __shfl_sync(0xffffffffu, f, part);
+      if (k0 + part < c.parts) add_part(v, w, k0 == 0 ? x[k] : output(k0 + part));
     }
-#pragma unroll
-    for (int d = kLanes / 2; d > 0; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
-    if (!real) continue;
-    const bool none = (g.causal ? n - q.T + t + 1 : n) <= 0;
-    const float inv = none ? 0.f : 1.0f / total;
-    const int64_t tok = q.row0 + t;
-    const int h = p.h * g.group + (r & 127) - in_tile * g.group;
-#pragma unroll
-    for (int v = 0; v < kVecs; ++v) {
-      const __nv_bfloat162 lo = __floats2bfloat162_rn(sum[v].x * inv, sum[v].y * inv), hi = __floats2bfloat162_rn(sum[v].z * inv, sum[v].w * inv);
-      uint2 bits;
-      bits.x = *reinterpret_cast<const uint32_t*>(&lo);
-      bits.y = *reinterpret_cast<const uint32_t*>(&hi);
-      *reinterpret_cast<uint2*>(o.out + tok * g.out_tok + h * g.out_head + (v * kLanes + l) * 4) = bits;
-    }
-    if (o.lse && l == 0) o.lse[tok * g.hq + h] = none ? -INFINITY : (top + log2f(total)) * 0.6931471805599453f;
   }
+#pragma unroll
+  for (int d = 16; d > 0; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
+  fold[warp][lane] = v;
+  __syncthreads();
+  if (warp != 0) return;
+#pragma unroll
+  for (int k = 1; k < kJoinWarps; ++k) add_part(v, 1.f, fold[k][lane]);
+  const int n = attend_len(as, g, c.p.i, status);
+  store_row(g, o, q.row0 + t, c.p.h * g.group + r - in_block * g.group, lane * 4, v, top, total, (g.causal ? n - q.T + t + 1 : n) <= 0);
+}
+
+// Many rows of a few parts: eight lanes take a row, all of them two parts at once, so that a warp does four rows in the time of one (a
+// warp per row and four rows after one another: 15 us of the 90 of 517 tokens over 8709 keys).
+__global__ void __launch_bounds__(kJoinWarps * 32)
+attend_join_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as, const AttendWs ws, int grid, const AttendOut o,
+                   DeviceStatus* status) {
+  constexpr int kLanes = 8, kVecs = 32 / kLanes;   // per row; 16-byte vectors of its output per lane
+  constexpr int kAhead = 2;                        // parts under way at once
+  static_assert(kLanes % kAhead == 0, "weights of kLanes parts at a time");
+  pdl_launch_dependents();
+  pdl_wait();
+  const int lane = threadIdx.x & 31, l = lane % kLanes;
+  const CutProblem c = cut_problem(g, as, ws, grid, blockIdx.x + 1);
+  if (c.parts == 0) return;
+  const AttendSeq q = as.seq[c.p.i];
+  const int r = (blockIdx.y * kJoinWarps + (threadIdx.x >> 5)) * (32 / kLanes) + lane / kLanes;
+  const int in_tile = (r & 127) / g.group, t = c.p.b * as.block_tokens + (r >> 7) * as.tile_tokens + in_tile;
+  const bool real = r < as.rows && in_tile < as.tile_tokens && t < q.T;
+  if (!__any_sync(0xffffffffu, real)) return;
+  auto output = [&](int k, int v) { return __ldcg(reinterpret_cast<const float4*>(ws.out + c.entry(as, k, r) * kHeadDim) + v * kLanes + l); };
+  auto stat = [&](int k) { return real && k < c.parts ? __ldcg(ws.stat + c.entry(as, k, r)) : make_float2(-INFINITY, 0.f); };
+  float4 x[kAhead][kVecs];
+  auto load = [&](int k0) {
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+      for (int v = 0; v < kVecs; ++v) x[k][v] = real && k0 + k < c.parts ? output(k0 + k, v) : make_float4(0.f, 0.f, 0.f, 0.f);
+  };
+  load(0);
+  const float2 first = stat(l);
+  float top = first.x;
+  for (int k = kLanes + l; k < c.parts; k += kLanes) top = fmaxf(top, stat(k).x);
+#pragma unroll
+  for (int d = kLanes / 2; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+  float total = 0.f;
+  float4 sum[kVecs];
+#pragma unroll
+  for (int v = 0; v < kVecs; ++v) sum[v] = make_float4(0.f, 0.f, 0.f, 0.f);
+  float f = 0.f;                                   // weight of part k0 + l of every kLanes parts
+  for (int k0 = 0; k0 < c.parts; k0 += kAhead) {
+    if (k0 > 0) load(k0);
+    if (k0 % kLanes == 0) {
+      const float2 st = k0 == 0 ? first : stat(k0 + l);
+      f = st.x == -INFINITY ? 0.f : ex2(st.x - top);
+      total += f * st.y;
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const float w = __shfl_sync(0xffffffffu, f, (k0 + k) % kLanes, kLanes);
+#pragma unroll
+      for (int v = 0; v < kVecs; ++v)
+        if (k0 + k < c.parts) add_part(sum[v], w, x[k][v]);
+    }
+  }
+#pragma unroll
+  for (int d = kLanes / 2; d > 0; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
+  if (!real) return;
+  const int n = attend_len(as, g, c.p.i, status);
+  const bool none = (g.causal ? n - q.T + t + 1 : n) <= 0;
+#pragma unroll
+  for (int v = 0; v < kVecs; ++v)
+    store_row(g, o, q.row0 + t, c.p.h * g.group + (r & 127) - in_tile * g.group, (v * kLanes + l) * 4, sum[v], top, total, none);
 }
 
 // The launches of a call: sequences with at most 16 query rows per KV head go to the kernel for few rows, the others to the
@@ -139,7 +201,6 @@ AttendPlans plan_attend(const CacheSeqs& cs, const CacheGeom& g, int sm_count) {
   AttendSeqs& few = p.rows.as;
   few.tile_shift = 6;
   static_assert(kRowsTile == 1 << 6 && kTcTile == 1 << 7, "tiles");
-  few.rows = kRowsMost;
   few.block_tokens = few.tile_tokens = std::max(1, kRowsMost / g.group);
   few.start_weight = 1;
   AttendSeqs& many = p.tc.as;
@@ -167,7 +228,9 @@ AttendPlans plan_attend(const CacheSeqs& cs, const CacheGeom& g, int sm_count) {
     as.seq[as.num] = AttendSeq{cs.new_off[s], T, cs.kv_len[s], (T + as.block_tokens - 1) / as.block_tokens};
     as.src[as.num++] = (uint8_t)s;
   }
-  // Rows that a block can have (a short chunk has fewer than two tiles of them).
+  // Rows that a block can have.
+  few.rows = 0;
+  for (int i = 0; i < few.num; ++i) few.rows = std::max(few.rows, few.seq[i].T * g.group);
   int64_t longest = 0;
   for (int i = 0; i < many.num; ++i) longest = std::max<int64_t>(longest, many.seq[i].T);
   if (longest <= many.tile_tokens) many.rows = ((int)longest * g.group + 31) / 32 * 32;
@@ -229,8 +292,8 @@ cudaError_t launch_attend_join(const Launch& L, const CacheGeom& g, const Attend
                                int grid, const AttendOut& o) {
   if (grid < 2) return cudaSuccess;
   const bool few = as.rows <= kRowsMost;
-  const int rows = kJoinWarps * (few ? 1 : 4);     // of a block at a time
-  auto kern = few ? attend_join_kernel<true> : attend_join_kernel<false>;
+  const int rows = few ? 1 : kJoinWarps * 4;       // of a block
+  auto kern = few ? attend_join_few_kernel : attend_join_kernel;
   return launch_pdl(kern, dim3((unsigned)(grid - 1), (unsigned)((as.rows + rows - 1) / rows)), dim3(kJoinWarps * 32), 0, L.stream, 1, g,
                     as, ws, grid, o, L.status);
 }
