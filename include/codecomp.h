@@ -351,7 +351,9 @@ typedef struct cc_cache_desc {
 int cc_rope_append(cc_ctx* ctx, const cc_cache_desc* desc, const void* q_new, const void* k_new,
                    const void* v_new, const int32_t* positions, void* q, void* k, void* v, void* stream);
 
-/* Bytes of device workspace (256-byte aligned) that cc_paged_attention needs.  0: invalid descriptor. */
+/* Bytes of device workspace (256-byte aligned) that cc_paged_attention needs for `desc`.  0: invalid descriptor.
+ * They do not grow with the lengths alone (they depend on how the work is cut up), but are never more than 266496 per
+ * SM (39.4 MB on a B200): a workspace of that size serves every descriptor. */
 size_t cc_attention_workspace_bytes(const cc_ctx* ctx, const cc_cache_desc* desc);
 
 /* Attention of the new tokens over the cache.  For new token t of sequence s and query head h, with the KV head

@@ -14,6 +14,8 @@ namespace cc {
 namespace {
 
 constexpr int kJoinWarps = 8;
+constexpr int kManyParts = 5;            // CTAs per problem from which on its parts are spread over warps,
+constexpr int kSpreadRows = 20;          // if its rows are no more than that per CTA of the attention
 
 // The join of the problems that are cut: blocks per (boundary between two shares, rows), idle unless the boundary is the first inside
 // its problem.  The parts of a problem follow each other in the order of the CTAs.
@@ -50,6 +52,33 @@ __device__ __forceinline__ CutProblem cut_problem(const CacheGeom& g, const Atte
       in = __ballot_sync(0xffffffffu, inside(place(s0 + lane)));
       c.parts += in == 0xffffffffu ? 32 : __ffs(~in) - 1;
       if (in != 0xffffffffu) break;
+    }
+  }
+  return c;
+}
+// The problem with index `at` in the list (heads outermost), found among all places; one whole warp.
+__device__ __forceinline__ CutProblem problem_at(const AttendSeqs& as, const AttendWs& ws, int grid, int at) {
+  const int lane = threadIdx.x & 31;
+  CutProblem c;
+  c.p = Place{at / as.blocks, 0, at % as.blocks, 0};
+  while (c.p.b >= as.seq[c.p.i].blocks) c.p.b -= as.seq[c.p.i++].blocks;
+  c.first = 0;
+  c.parts = 0;
+  for (int s0 = 0; s0 < grid; s0 += 5 * 32) {      // (five loads under way: as many as there are SMs)
+    int4 x[5];
+#pragma unroll
+    for (int k = 0; k < 5; ++k) {
+      const int share = s0 + k * 32 + lane;
+      x[k] = share < grid ? __ldcg(reinterpret_cast<const int4*>(ws.place + share)) : make_int4(0, 0, 0, -1);
+    }
+#pragma unroll
+    for (int k = 0; k < 5; ++k) {
+      const unsigned in = __ballot_sync(0xffffffffu, x[k].w > 0 && x[k].x == c.p.h && x[k].y == c.p.i && x[k].z == c.p.b);
+      if (in && c.parts == 0) {
+        c.first = s0 + k * 32 + __ffs(in) - 1;
+        c.parts = 1;
+      }
+      c.parts += __popc(in);
     }
   }
   return c;
@@ -118,6 +147,89 @@ attend_join_few_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
   for (int k = 1; k < kJoinWarps; ++k) add_part(v, 1.f, fold[k][lane]);
   const int n = attend_len(as, g, c.p.i, status);
   store_row(g, o, q.row0 + t, c.p.h * g.group + r - in_block * g.group, lane * 4, v, top, total, (g.causal ? n - q.T + t + 1 : n) <= 0);
+}
+
+// Many parts of few problems: a block takes four rows of a problem, eight lanes a row, each of its warps every eighth part (38 tokens
+// over 18246 keys, 2 KV heads, 37 parts: 30.6 -> 20.2 us).  Every block looks through all places, so it loses where there are many of
+// them: 219 tokens in two sequences, 28 problems of 256 rows in five parts, 26.7 -> 36.9 us.
+__global__ void __launch_bounds__(kJoinWarps * 32)
+attend_join_spread_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as, const AttendWs ws, int grid, const AttendOut o,
+                          DeviceStatus* status) {
+  constexpr int kLanes = 8, kVecs = 32 / kLanes, kAhead = 2;
+  __shared__ float4 fold[kJoinWarps][4][32];
+  __shared__ float2 stats[4];
+  pdl_launch_dependents();
+  pdl_wait();
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, l = lane % kLanes;
+  const CutProblem c = problem_at(as, ws, grid, blockIdx.x);
+  if (c.parts == 0) return;
+  const AttendSeq q = as.seq[c.p.i];
+  auto token = [&](int r) {                        // of the sequence, -1: the block of tokens has no such row
+    const int in_tile = (r & 127) / g.group, t = c.p.b * as.block_tokens + (r >> 7) * as.tile_tokens + in_tile;
+    return r < as.rows && in_tile < as.tile_tokens && t < q.T ? t : -1;
+  };
+  const int r = blockIdx.y * 4 + lane / kLanes;
+  const bool real = token(r) >= 0;
+  if (!__any_sync(0xffffffffu, real)) return;      // (the same four rows in all warps)
+  auto output = [&](int k, int v) { return __ldcg(reinterpret_cast<const float4*>(ws.out + c.entry(as, k, r) * kHeadDim) + v * kLanes + l); };
+  auto stat = [&](int k) { return real && k < c.parts ? __ldcg(ws.stat + c.entry(as, k, r)) : make_float2(-INFINITY, 0.f); };
+  float4 x[kAhead][kVecs];
+  auto load = [&](int k0) {
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+      for (int v = 0; v < kVecs; ++v) {
+        const int part = k0 + k * kJoinWarps;
+        x[k][v] = real && part < c.parts ? output(part, v) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+  };
+  load(warp);
+  float2 st[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) st[k] = stat(l + k * kLanes);
+  float top = fmaxf(fmaxf(st[0].x, st[1].x), fmaxf(st[2].x, st[3].x));
+  for (int k = 32 + l; k < c.parts; k += kLanes) top = fmaxf(top, stat(k).x);
+#pragma unroll
+  for (int d = kLanes / 2; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+  float total = 0.f;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) total += st[k].x == -INFINITY ? 0.f : st[k].y * ex2(st[k].x - top);
+  for (int k = 32 + l; k < c.parts; k += kLanes) {
+    const float2 y = stat(k);
+    total += y.x == -INFINITY ? 0.f : y.y * ex2(y.x - top);
+  }
+#pragma unroll
+  for (int d = kLanes / 2; d > 0; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
+  float4 sum[kVecs];
+#pragma unroll
+  for (int v = 0; v < kVecs; ++v) sum[v] = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int k0 = warp; k0 < c.parts; k0 += kAhead * kJoinWarps) {
+    float w[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const float m = stat(k0 + k * kJoinWarps).x;
+      w[k] = m == -INFINITY ? 0.f : ex2(m - top);
+    }
+    if (k0 > warp) load(k0);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+#pragma unroll
+      for (int v = 0; v < kVecs; ++v)
+        if (k0 + k * kJoinWarps < c.parts) add_part(sum[v], w[k], x[k][v]);
+  }
+#pragma unroll
+  for (int v = 0; v < kVecs; ++v) fold[warp][lane / kLanes][v * kLanes + l] = sum[v];
+  if (warp == 0 && l == 0) stats[lane / kLanes] = make_float2(top, total);
+  __syncthreads();
+  if (warp >= 4) return;
+  const int t = token(blockIdx.y * 4 + warp);      // a warp per row now
+  if (t < 0) return;
+  float4 v = fold[0][warp][lane];
+#pragma unroll
+  for (int k = 1; k < kJoinWarps; ++k) add_part(v, 1.f, fold[k][warp][lane]);
+  const int row = blockIdx.y * 4 + warp, n = attend_len(as, g, c.p.i, status);
+  store_row(g, o, q.row0 + t, c.p.h * g.group + (row & 127) % g.group, lane * 4, v, stats[warp].x, stats[warp].y,
+            (g.causal ? n - q.T + t + 1 : n) <= 0);
 }
 
 // Many rows of a few parts: eight lanes take a row, all of them two parts at once, so that a warp does four rows in the time of one (a
@@ -189,12 +301,35 @@ struct AttendPlan {
   AttendSeqs as;
   int grid;
 };
-constexpr int kSplit = 4;
 constexpr int64_t kFewKeys = 400000;      // (keys x KV heads)
 struct AttendPlans {
   AttendPlan rows, tc;
   bool too_much;                                   // 2^31 tiles and more
 };
+
+// Fewer problems than SMs in the tensor-core kernel: the number of CTAs for each of them, or 0: shares by weight, which even out problems
+// of different lengths but give a CTA the end of one and the beginning of another.  What a choice takes, in tenths of a us: the
+// longest share's steps of 128 keys, a second start (shares by weight), the join and its parts; fitted to 90 random batches timed with
+// every number: 1.4 % below shares by weight on average, with 1 each and no join 504 tokens in three sequences over 251 to
+// 848 keys 24.2 -> 19.2 us, 4 % above at worst.
+int ctas_each(const CacheGeom& g, const AttendSeqs& as, int64_t total, int* grid) {
+  constexpr int64_t kStep = 17, kStart = 50, kJoin = 50, kJoinPart = 1;
+  const int64_t problems = (int64_t)as.blocks * g.hkv;
+  if (problems > *grid) return 0;
+  int64_t most = 0;
+  for (int i = 0; i < as.num; ++i) most = std::max<int64_t>(most, (as.seq[i].n + (1 << as.tile_shift) - 1) >> as.tile_shift);
+  int best = 0;
+  int64_t least = (total + *grid - 1) / *grid * kStep + kStart + *grid / problems * kJoinPart;
+  for (int64_t each = 1; each * problems <= *grid && each <= std::max<int64_t>(1, most); ++each) {
+    const int64_t time = (most + each - 1) / each * kStep + (each > 1 ? kJoin + each * kJoinPart : 0);
+    if (time < least) {
+      least = time;
+      best = (int)each;
+    }
+  }
+  if (best > 0) *grid = (int)(best * problems);
+  return best;
+}
 
 AttendPlans plan_attend(const CacheSeqs& cs, const CacheGeom& g, int sm_count) {
   AttendPlans p = {};
@@ -245,22 +380,8 @@ AttendPlans plan_attend(const CacheSeqs& cs, const CacheGeom& g, int sm_count) {
     total *= g.hkv;
     if (total >> 31) p.too_much = true;
     x->grid = (int)std::min<int64_t>(total, sm_count);
-    // Fewer problems than SMs, and all alike: as many CTAs for each.  A CTA then has part of one problem instead of the end of one and
-    // the beginning of another, which costs it a start and an end (kSplit tiles; 517 tokens over 8709 keys 96 -> 90 us).
-    int64_t problems = 0, most = 0, least = INT64_MAX;
-    for (int i = 0; i < as.num; ++i) {
-      const int64_t n = as.seq[i].n, first = g.causal ? std::max<int64_t>(0, n - as.seq[i].T) : n;
-      problems += (int64_t)as.seq[i].blocks * g.hkv;
-      most = std::max(most, (n + (1 << as.tile_shift) - 1) >> as.tile_shift);
-      least = std::min(least, first >> as.tile_shift);
-    }
-    if (x == &p.tc && problems > 0 && problems <= x->grid) {
-      const int64_t each = x->grid / problems;
-      if (least >= 2 * each && most / each < total / x->grid + kSplit) {
-        x->as.each = (int)each;
-        x->grid = (int)(each * problems);
-      }
-    }
+    for (int i = 0; i < as.num; ++i) x->as.blocks += as.seq[i].blocks;
+    if (x == &p.tc && as.num > 0) x->as.each = ctas_each(g, x->as, total, &x->grid);
   }
   return p;
 }
@@ -294,10 +415,17 @@ CUresult encode_queries(EncodeTiledFn encode, const CacheSeqs& cs, const CacheGe
 cudaError_t launch_attend_join(const Launch& L, const CacheGeom& g, const AttendSeqs& as, const AttendWs& ws,
                                int grid, const AttendOut& o) {
   if (grid < 2) return cudaSuccess;
-  const bool few = as.rows <= kRowsMost;
-  const int rows = few ? 1 : kJoinWarps * 4;       // of a block
-  auto kern = few ? attend_join_few_kernel : attend_join_kernel;
-  return launch_pdl(kern, dim3((unsigned)(grid - 1), (unsigned)((as.rows + rows - 1) / rows)), dim3(kJoinWarps * 32), 0, L.stream, 1, g,
+  if (as.each == 1) return cudaSuccess;            // no problem is cut
+  const dim3 threads(kJoinWarps * 32);
+  if (as.rows <= kRowsMost)
+    return launch_pdl(attend_join_few_kernel, dim3((unsigned)(grid - 1), (unsigned)as.rows), threads, 0, L.stream, 1, g, as, ws, grid, o,
+                      L.status);
+  const int64_t problems = (int64_t)as.blocks * g.hkv;
+  if (problems * kManyParts <= grid && problems * as.rows <= (int64_t)kSpreadRows * grid)
+    return launch_pdl(attend_join_spread_kernel, dim3((unsigned)problems, (unsigned)((as.rows + 3) / 4)), threads, 0, L.stream, 1, g, as, ws,
+                      grid, o, L.status);
+  const int rows = kJoinWarps * 4;
+  return launch_pdl(attend_join_kernel, dim3((unsigned)(grid - 1), (unsigned)((as.rows + rows - 1) / rows)), threads, 0, L.stream, 1, g,
                     as, ws, grid, o, L.status);
 }
 

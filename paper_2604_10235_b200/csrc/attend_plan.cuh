@@ -26,6 +26,7 @@ struct AttendSeqs {            // the sequences of one launch
   int start_weight;            // weight of a problem's start, in tiles (at least 1)
   int rows;                    // rows of a block (and of a partial result)
   int each;                    // > 0: no shares by weight, every problem has that many CTAs
+  int blocks;                  // of all sequences
   AttendSeq seq[CC_MAX_SEQS];
   uint8_t src[CC_MAX_SEQS];    // index of the sequence in the call
 };

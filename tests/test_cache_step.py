@@ -221,3 +221,18 @@ def test_typed_arguments_are_checked():
         fork(at, desc, -1, 1, [None], [bf], parents, 2, i32, 3, i32, 0)
     with pytest.raises((TypeError, BufferError)):
         fork(at, desc, -1, 1, [bf], [bf], [0, 5], 2, i32, 3, i32, 0)
+
+
+def test_one_workspace_for_all_lengths():
+    """What the header promises: no more than 266496 bytes per SM, whatever the batch."""
+    rng = np.random.default_rng(3)
+    for _ in range(2000):
+        seqs = int(rng.integers(1, 65))
+        lens = np.exp(rng.uniform(0, math.log(200000), seqs)).astype(np.int32)
+        c = Call(lens, np.minimum(lens, np.exp(rng.uniform(0, math.log(4000), seqs)).astype(np.int32)))
+        c.d.n_heads_kv = int(rng.choice([1, 2, 4, 8, 32]))
+        c.d.n_heads_q = c.d.n_heads_kv * int(rng.choice([1, 4, 7, 16]))
+        c.d.page_table_stride = 200000 // 16
+        sms = int(rng.choice([1, 2, 20, 148]))
+        c.ctx = C.create_string_buffer(bytes(4) + sms.to_bytes(4, "little") + bytes(4088), 4096)
+        assert 256 <= c.lib.cc_attention_workspace_bytes(c.ctx, C.byref(c.d)) <= 266496 * sms

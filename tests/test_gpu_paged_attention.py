@@ -344,3 +344,27 @@ def test_out_off_the_32_byte_grid():
         assert ctx().poll() == 0
         assert_attention(out, None, attend_reference(cache, q, [new]))
         assert (big[:8] == 9.0).all()
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("hq,hkv,new,lens", [
+    (8, 2, [92], [256]), (32, 8, [26, 227, 251], [848, 655, 251]),            # a problem per CTA
+    (28, 4, [41], [571]), (8, 2, [84], [728]),                               # a few CTAs per problem
+    (8, 2, [300], [300]), (8, 2, [180], [40]),                               # blocks with fewer tiles than CTAs, or none
+    (8, 2, [40, 40], [5000, 0]), (8, 2, [40, 70], [5000, 1]),
+    (8, 2, [44, 31], [454, 16271]), (28, 4, [27], [9151]), (5, 1, [130], [14000])])      # many parts of a problem
+def test_few_problems(hq, hkv, new, lens, causal):
+    check(Cache(lens, hkv, 16, seed=len(new) + lens[0]), hq, new, causal)
+
+
+@pytest.mark.parametrize("new", [[38], [90], [90, 3]])
+def test_few_problems_shorter_on_the_device(new):
+    cache = Cache([9000] * len(new), 2, 16, seed=31)
+    now = torch.zeros(len(new), dtype=torch.int32, device="cuda")
+    desc = cache.desc(8, new, dev_kv_lens=now)
+    ws = ctx().cache_workspace(desc)
+    for n in (9000, 0, 1, 128, 129, 1000, 8999):
+        now.fill_(n)
+        q, out, lse = attend(ctx(), cache, 8, new, desc=desc, ws=ws)
+        assert ctx().poll() == 0
+        assert_attention(out, lse, attend_reference(cache, q, new, lens=now.tolist()))
