@@ -372,7 +372,8 @@ int cc_paged_attention(cc_ctx* ctx, const cc_cache_desc* desc, const void* q, co
  * one geometry; the page table is common to the layers).  parents: HOST [n_children], n_children at most
  * CC_MAX_CHILDREN.  child_table: device i32 [n_children][child_table_stride], child_table_stride at least the
  * pages of every parent; it may lie in the array of page_table as long as no child's row is a parent's.
- * free_pages: device i32 [n_children], different pages that no sequence uses. */
+ * free_pages: device i32 [n_children], different pages that no sequence uses.  No layers or no children: nothing is
+ * done, child_table stays as it is. */
 #define CC_MAX_CHILDREN 256
 int cc_fork_pages(cc_ctx* ctx, const cc_cache_desc* desc, int32_t n_layers, void* const* k, void* const* v,
                   const int32_t* parents, int32_t n_children, int32_t* child_table,

@@ -150,7 +150,7 @@ attend_join_few_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
 }
 
 // Many parts of few problems: a block takes four rows of a problem, eight lanes a row, each of its warps every eighth part (38 tokens
-// over 18246 keys, 2 KV heads, 37 parts: 30.6 -> 20.2 us).  Every block looks through all places, so it loses where there are many of
+// over 18246 keys, 2 KV heads: 30.6 -> 20.2 us).  Every block looks through all places, so it loses where there are many of
 // them: 219 tokens in two sequences, 28 problems of 256 rows in five parts, 26.7 -> 36.9 us.
 __global__ void __launch_bounds__(kJoinWarps * 32)
 attend_join_spread_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as, const AttendWs ws, int grid, const AttendOut o,

@@ -3,7 +3,7 @@
 //   o_r = sum_j p_rj v_j / sum_j p_rj,   p_rj = exp(scale q_r . k_j - reference_r)
 //
 // Every row of K and V is read once and 4 flops are done with each of its bytes per query row: bound by HBM (64 sequences, 245 k
-// keys, 8 heads, 1.0 GB: 156 us, 6.4 TB/s), few keys by latency (2305 keys x 8 heads 10.9 us, of which the kernel 5).  The matrix
+// keys, 8 heads, 1.0 GB: 156 to 165 us, 6.1 to 6.4 TB/s), few keys by latency (2305 keys x 8 heads 10.0 to 11.0 us, of which the kernel 5).  The matrix
 // instructions are mma.sync (m16n8k16): the 16 rows are their M side, against at least 64 of tcgen05.mma, and a tile's 32 per
 // scheduler, some 500 clocks, fit well into the 1400 that its 32 KB take at this SM's share of the bandwidth.  The tensor-core
 // kernel takes 213 us for the same.
