@@ -280,7 +280,8 @@ int cc_select_chunks(cc_ctx* ctx, const float* score, int32_t num_chunks, int32_
  *    k, v              bf16 page pool [pool_pages * page_size][H_kv][d]: slot j of sequence s is row
  *                      page_table[s][j / page_size] * page_size + j % page_size.  Sequences may share pages.
  * Only the first ceil(n_s / page_size) entries of a row of the page table are read.  A page id outside
- * [0, pool_pages) is skipped and flagged (CC_ERR_DEVICE_FLAG in the status word).
+ * [0, pool_pages) is skipped and flagged (CC_ERR_DEVICE_FLAG in the status word): tokens are not appended to its
+ * slots, no token attends to them, forks neither copy nor name it.
  *
  * Lengths on the device.  With dev_kv_lens, n_s is read there when the work runs and kv_lens holds an upper
  * bound of each, so that a captured graph can be replayed while its sequences grow; a value outside
@@ -359,9 +360,10 @@ size_t cc_attention_workspace_bytes(const cc_ctx* ctx, const cc_cache_desc* desc
 /* Attention of the new tokens over the cache.  For new token t of sequence s and query head h, with the KV head
  * h / (H_q / H_kv), over the slots j that it attends to (all, or those up to n_s - T_s + t):
  *   out = sum_j softmax_j(scale * q . k_j) v_j,   lse = log sum_j exp(scale * q . k_j).
- * A token that attends to no slot gets out = 0 and lse = -inf.  lse may be NULL.  bf16 operands, f32 products, sums
- * and softmax, probabilities rounded to bf16 for the product with v, one rounding of the result.  Rows of k and v
- * beyond n_s are never used, whatever they hold.  out must not overlap q, k or v. */
+ * A token that attends to no slot (none, or slots on missing pages alone) gets out = 0 and lse = -inf.  lse may be
+ * NULL.  bf16 operands, f32 products, sums and softmax, probabilities rounded to bf16 for the product with v, one
+ * rounding of the result.  Rows of k and v beyond n_s are never used, whatever they hold.  out must not overlap q, k
+ * or v. */
 int cc_paged_attention(cc_ctx* ctx, const cc_cache_desc* desc, const void* q, const void* k,
                        const void* v, void* out, float* lse, void* ws, size_t ws_bytes, void* stream);
 

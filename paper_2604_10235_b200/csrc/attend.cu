@@ -146,7 +146,9 @@ attend_join_few_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
 #pragma unroll
   for (int k = 1; k < kJoinWarps; ++k) add_part(v, 1.f, fold[k][lane]);
   const int n = attend_len(as, g, c.p.i, status);
-  store_row(g, o, q.row0 + t, c.p.h * g.group + r - in_block * g.group, lane * 4, v, top, total, (g.causal ? n - q.T + t + 1 : n) <= 0);
+  const int slots = g.causal ? n - q.T + t + 1 : n;
+  store_row(g, o, q.row0 + t, c.p.h * g.group + r - in_block * g.group, lane * 4, v, top, total,
+            slots <= 0 || (total == 0.f && attend_no_slot(as, g, c.p.i, slots)));
 }
 
 // Many parts of few problems: a block takes four rows of a problem, eight lanes a row, each of its warps every eighth part (38 tokens
@@ -227,9 +229,9 @@ attend_join_spread_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs 
   float4 v = fold[0][warp][lane];
 #pragma unroll
   for (int k = 1; k < kJoinWarps; ++k) add_part(v, 1.f, fold[k][warp][lane]);
-  const int row = blockIdx.y * 4 + warp, n = attend_len(as, g, c.p.i, status);
+  const int row = blockIdx.y * 4 + warp, n = attend_len(as, g, c.p.i, status), slots = g.causal ? n - q.T + t + 1 : n;
   store_row(g, o, q.row0 + t, c.p.h * g.group + (row & 127) % g.group, lane * 4, v, stats[warp].x, stats[warp].y,
-            (g.causal ? n - q.T + t + 1 : n) <= 0);
+            slots <= 0 || (stats[warp].y == 0.f && attend_no_slot(as, g, c.p.i, slots)));
 }
 
 // Many rows of a few parts: eight lanes take a row, all of them two parts at once, so that a warp does four rows in the time of one (a
@@ -288,8 +290,8 @@ attend_join_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as, con
 #pragma unroll
   for (int d = kLanes / 2; d > 0; d >>= 1) total += __shfl_xor_sync(0xffffffffu, total, d);
   if (!real) return;
-  const int n = attend_len(as, g, c.p.i, status);
-  const bool none = (g.causal ? n - q.T + t + 1 : n) <= 0;
+  const int n = attend_len(as, g, c.p.i, status), slots = g.causal ? n - q.T + t + 1 : n;
+  const bool none = slots <= 0 || (total == 0.f && attend_no_slot(as, g, c.p.i, slots));
 #pragma unroll
   for (int v = 0; v < kVecs; ++v)
     store_row(g, o, q.row0 + t, c.p.h * g.group + (r & 127) - in_tile * g.group, (v * kLanes + l) * 4, sum[v], top, total, none);
@@ -388,15 +390,15 @@ AttendPlans plan_attend(const CacheSeqs& cs, const CacheGeom& g, int sm_count) {
 
 // A page (or as many of its tokens as a tile has), both halves of the channels, one head, in one copy: in shared memory
 // groups of eight tokens of 2 KB each, the eight rows of channels 0-63 followed by those of channels 64-127.
-CUresult encode_pool(EncodeTiledFn encode, const CacheGeom& g, const void* p, int tile_keys, CUtensorMap* map) {
+// `fill`: what a copy from behind the pool brings.
+CUresult encode_pool(EncodeTiledFn encode, const CacheGeom& g, const void* p, int tile_keys, CUtensorMapFloatOOBfill fill, CUtensorMap* map) {
   const cuuint32_t estr[5] = {1, 1, 1, 1, 1};
   const cuuint64_t rows = (cuuint64_t)g.pool_pages << g.page_shift;
   const cuuint64_t dims[5] = {64, 8, 2, rows / 8, (cuuint64_t)g.hkv};
   const cuuint64_t strides[4] = {(cuuint64_t)g.kv_tok * 2, 128, (cuuint64_t)g.kv_tok * 16, (cuuint64_t)g.kv_head * 2};
   const cuuint32_t box[5] = {64, 8, 2, (cuuint32_t)(std::min(1 << g.page_shift, tile_keys) / 8), 1};
   return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 5, const_cast<void*>(p), dims, strides, box, estr,
-                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+                CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, fill);
 }
 
 // The tokens of a tile, the heads of a group, half of the channels: rows token * group + head of 128 bytes.
@@ -444,8 +446,8 @@ cudaError_t launch_attend(const Launch& L, const CacheSeqs& cs, const CacheGeom&
   if (p.too_much) return cudaErrorInvalidConfiguration;
   CUtensorMap q_map, k_map, v_map;
   auto pools = [&](int tile_keys) {
-    CUresult r = encode_pool(encode, g, k, tile_keys, &k_map);
-    if (r == CUDA_SUCCESS) r = encode_pool(encode, g, v, tile_keys, &v_map);
+    CUresult r = encode_pool(encode, g, k, tile_keys, CU_TENSOR_MAP_FLOAT_OOB_FILL_NAN_REQUEST_ZERO_FMA, &k_map);
+    if (r == CUDA_SUCCESS) r = encode_pool(encode, g, v, tile_keys, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE, &v_map);
     *drv_err = (int)r;
     return r == CUDA_SUCCESS;
   };

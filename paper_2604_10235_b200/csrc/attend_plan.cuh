@@ -223,6 +223,32 @@ struct AttendWalk {
   __device__ __forceinline__ int slot() const { return 2 * (int)blockIdx.x + (t0 == 0 ? 1 : 0); }
 };
 
+// Slots on a page that is not one of the pool take no part.  Their copies start behind the pool's last row, where the map of K gives no
+// numbers and that of V zeros: logits that are no numbers are what the kernels look for anyway, so that only then a
+// warp asks the page table.  (Over 57 batches of keys that are all there 0.5 % on average; 2.4 % with an entry per tile that says which keys
+// are missing and that every warp reads.)
+__device__ __forceinline__ int copy_group(const CacheGeom& g, bool good, int page, int in_page) {       // first group of eight rows
+  return good ? (int)((((int64_t)page << g.page_shift) + in_page) >> 3) : (int)(((int64_t)g.pool_pages << g.page_shift) >> 3);
+}
+// Groups of eight keys of the sequence from key0 (a multiple of eight) on that are missing, a bit each; one whole warp.
+__device__ __forceinline__ uint32_t missing_groups(const AttendSeqs& as, const CacheGeom& g, int i, int key0, int groups, int limit) {
+  const int lane = threadIdx.x & 31, key = key0 + lane * 8;
+  int page = 0;
+  if (lane < groups && key < limit) page = g.table[(int64_t)as.src[i] * g.table_stride + (key >> g.page_shift)];
+  return __ballot_sync(0xffffffffu, page < 0 || page >= g.pool_pages);
+}
+// Whether none of the first `lim` slots of a sequence lies on a page of the pool.  Asked where a row's sum is zero: a reference is a logit
+// of its row and gives 1, so such a row had no slot, or logits of minus infinity alone (whose softmax is no number).
+__device__ __forceinline__ bool attend_no_slot(const AttendSeqs& as, const CacheGeom& g, int i, int lim) {
+  const int32_t* table = g.table + (int64_t)as.src[i] * g.table_stride;
+#pragma unroll 1
+  for (int p = 0; (p << g.page_shift) < lim; ++p) {
+    const int page = table[p];
+    if (page >= 0 && page < g.pool_pages) return false;
+  }
+  return true;
+}
+
 // Pairs of bf16: a mask of the finite ones, and whether any of eight is infinite or no number.
 __device__ __forceinline__ uint32_t odd_halves(uint32_t two) { return ((two & 0x7f807f80u) + 0x00800080u) & 0x80008000u; }
 __device__ __forceinline__ uint32_t finite_halves(uint32_t two) {

@@ -60,6 +60,11 @@ __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], 
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float d;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(d) : "f"(a), "f"(b));
+  return d;
+}
 __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   uint32_t r;
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -142,9 +147,8 @@ attend_rows_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
         if (!bounded_wait(pipe, &sh->empty[stage], phase ^ 1, CC_ERR_TIMEOUT, 71)) { ok = false; break; }
         const bool good = mine && id >= 0 && id < g.pool_pages;
         if (mine && !good) report_error(status, CC_ERR_DEVICE_FLAG, 620);
-        const unsigned mask = __ballot_sync(0xffffffffu, good);
-        // first group of eight rows of the copy
-        const int group8 = (int)((((int64_t)id << g.page_shift) + (key & ((1 << g.page_shift) - 1))) >> 3);
+        const unsigned mask = __ballot_sync(0xffffffffu, mine);
+        const int group8 = copy_group(g, good, id, key & ((1 << g.page_shift) - 1));
         const uint32_t fb = smem_u32(&sh->full[stage]);
         const uint32_t dst = smem_u32(ring) + (uint32_t)stage * 2 * kTileBytes;
         if (elected) mbar_expect_tx(fb, (uint32_t)__popc(mask) * 2u * copy_bytes);
@@ -231,11 +235,24 @@ attend_rows_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
               x[i][e] = sc[e >> 1][2 * i + (e & 1)] * c2;
               if (edge && key0 + 2 * (lane & 3) + (e & 1) + 8 * (e >> 1) >= lim[i]) x[i][e] = -INFINITY;
             }
-            top[i] = fmaxf(fmaxf(x[i][0], x[i][1]), fmaxf(x[i][2], x[i][3]));
-            top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
-            top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
+            top[i] = max_nan(max_nan(x[i][0], x[i][1]), max_nan(x[i][2], x[i][3]));
+            top[i] = max_nan(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
+            top[i] = max_nan(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
           }
-          if (__any_sync(0xffffffffu, top[0] > ref[0] + kSlack || top[1] > ref[1] + kSlack)) {
+          if (__any_sync(0xffffffffu, !(top[0] <= ref[0] + kSlack && top[1] <= ref[1] + kSlack))) {
+            if (__builtin_expect(__any_sync(0xffffffffu, top[0] != top[0] || top[1] != top[1]), 0)) {
+              const uint32_t lost = missing_groups(as, g, w.at.i, key0, 2, most);
+#pragma unroll
+              for (int i = 0; i < 2; ++i) {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                  if (lost >> (e >> 1) & 1u) x[i][e] = -INFINITY;
+                // (a logit that is no number is not a reference)
+                top[i] = fmaxf(fmaxf(x[i][0], x[i][1]), fmaxf(x[i][2], x[i][3]));
+                top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 1));
+                top[i] = fmaxf(top[i], __shfl_xor_sync(0xffffffffu, top[i], 2));
+              }
+            }
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
               const float up = fmaxf(ref[i], top[i]);
@@ -338,7 +355,8 @@ attend_rows_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
         if (whole) {
           const int t = r / g.group, h = w.at.h * g.group + r - t * g.group;
           const int64_t tok = w.q.row0 + tok0 + t;
-          const bool none = (g.causal ? w.q.n - w.q.T + tok0 + t + 1 : w.q.n) <= 0;       // no key
+          const int slots = g.causal ? w.q.n - w.q.T + tok0 + t + 1 : w.q.n;
+          const bool none = slots <= 0 || (total == 0.f && attend_no_slot(as, g, w.at.i, slots));
           const float inv = none ? 0.f : 1.0f / total;
           *reinterpret_cast<uint2*>(o.out + tok * g.out_tok + h * g.out_head + c) =
               make_uint2(pack_bf16(v.x * inv, v.y * inv), pack_bf16(v.z * inv, v.w * inv));

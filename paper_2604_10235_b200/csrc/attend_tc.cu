@@ -129,6 +129,23 @@ __device__ __forceinline__ void raise(float high, bool real, float& ref, uint64_
     }
   }
 }
+// Writes minus infinity over the logits of missing keys (groups of eight, a bit each), from chunk `from` of 32 keys on; the maximum of
+// the chunks' first `last` keys.
+__device__ __forceinline__ float mask_missing(uint32_t s_addr, int from, int last, uint32_t lost, uint32_t (&v)[32]) {
+  float high = -INFINITY;
+#pragma unroll 1
+  for (int c = from; c < 4; ++c) {
+    tmem_ld32(s_addr + c * 32, v);
+    tmem_wait_ld();
+#pragma unroll
+    for (int e = 0; e < 32; ++e)
+      if (c * 32 + e >= last || (lost >> (c * 4 + (e >> 3)) & 1u)) v[e] = 0xff800000u;
+    tmem_st32(s_addr + c * 32, v);
+    high = max3_nan(high, max32_nan(v), high);
+  }
+  tmem_wait_st();
+  return high;
+}
 // Half of a tile of P is complete.
 __device__ __forceinline__ void hand_over(uint32_t bar, int lane) {
   tmem_wait_st();
@@ -205,8 +222,8 @@ attend_tc_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
         if (mine) page = table[key >> g.page_shift];
         const bool good = mine && page >= 0 && page < g.pool_pages;
         if (mine && !good) report_error(status, CC_ERR_DEVICE_FLAG, 621);
-        const unsigned mask = __ballot_sync(0xffffffffu, good);
-        const int group8 = (int)(((int64_t)page << g.page_shift) >> 3);
+        const unsigned mask = __ballot_sync(0xffffffffu, mine);
+        const int group8 = copy_group(g, good, page, 0);
 #pragma unroll 1
         for (int kv = 0; kv < 2; ++kv) {
           if (!wait(&sh->empty[stage], phase ^ 1, 81)) { ok = false; break; }
@@ -421,8 +438,9 @@ attend_tc_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
             }
           }
           if (from < 4) {
-            // The maximum first: tiles with masked keys, logits far above the reference.
+            // The maximum first: tiles with masked keys, logits far above the reference or no numbers, missing keys among the latter.
             const int last = t >= plain ? lim - key0 : kTcTile;
+            if (t == w.t0 && from == 0) ref = -INFINITY;
             float high = -INFINITY;
             uint32_t v[32];
 #pragma unroll 1
@@ -436,6 +454,8 @@ attend_tc_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
               }
               high = max3_nan(high, max32_nan(v), high);
             }
+            if (__builtin_expect(__any_sync(0xffffffffu, real && high != high), 0))
+              high = mask_missing(s_addr, from, last, missing_groups(as, g, w.at.i, key0, kTcTile / 8, w.limit), v);
             raise(high * c2, real, ref, sum, t > w.t0 || from > 0, o_addr);
             const uint64_t off2 = offset_of(ref);
             float reach = 0.f;
@@ -469,11 +489,16 @@ attend_tc_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
       }
       const float total = total_of(sum);
       const bool whole = w.whole();
+      bool none = lim <= 0;
+      if (__builtin_expect(__any_sync(0xffffffffu, whole && !none && total == 0.f), 0)) {
+        if (total == 0.f) none = attend_no_slot(as, g, w.at.i, lim);
+        __syncwarp();
+      }
       const int h = w.at.h * g.group + r - in_tile * g.group;
       const int64_t row = w.q.row0 + tok, at = (int64_t)w.slot() * as.rows + i * 128 + r;
       if (!dead && !idle) {
-        const float inv = lim <= 0 ? 0.f : 1.0f / total;
-        if (real && whole && o.lse) o.lse[row * g.hq + h] = lim <= 0 ? -INFINITY : (ref + log2f(total)) * kLn2;
+        const float inv = none ? 0.f : 1.0f / total;
+        if (real && whole && o.lse) o.lse[row * g.hq + h] = none ? -INFINITY : (ref + log2f(total)) * kLn2;
         if (real && !whole) ws.stat[at] = make_float2(ref, total);
 #pragma unroll 1
         for (int c = 0; c < 4; ++c) {
@@ -506,7 +531,7 @@ attend_tc_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
             uint32_t y[16];
 #pragma unroll
             for (int e = 0; e < 16; ++e)
-              y[e] = lim <= 0 ? 0u : pack_bf16(__uint_as_float(x[2 * e]) * inv, __uint_as_float(x[2 * e + 1]) * inv);
+              y[e] = none ? 0u : pack_bf16(__uint_as_float(x[2 * e]) * inv, __uint_as_float(x[2 * e + 1]) * inv);
             if (o.wide) {
               store32(dst, y);
               store32(dst + 16, y + 8);
