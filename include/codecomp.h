@@ -369,8 +369,9 @@ int cc_paged_attention(cc_ctx* ctx, const cc_cache_desc* desc, const void* q, co
 
 /* Forks sequences: child f continues sequence parents[f].  Its row of child_table names the parent's full pages
  * (shared from now on) and, where the parent's last page is not full, the fresh page free_pages[f], which receives
- * the rows of that page up to n_s in every layer; the remaining entries become -1.  free_pages[f] of a child
- * whose parent ends with a full page is not used.  k, v: HOST arrays of n_layers device pointers (page pools of
+ * the rows of that page up to n_s in every layer; the remaining entries become -1, and so does that of a page whose
+ * id, in the parent's row or in free_pages, is outside the pool.  free_pages[f] of a child whose parent ends with a
+ * full page is not used.  k, v: HOST arrays of n_layers device pointers (page pools of
  * one geometry; the page table is common to the layers).  parents: HOST [n_children], n_children at most
  * CC_MAX_CHILDREN.  child_table: device i32 [n_children][child_table_stride], child_table_stride at least the
  * pages of every parent; it may lie in the array of page_table as long as no child's row is a parent's.

@@ -23,6 +23,8 @@ fork_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, const __gri
   const int32_t* parent_row = g.table + (int64_t)s * g.table_stride;
   const int fresh = rest > 0 ? A.free_pages[child] : -1;
   const bool fresh_ok = fresh >= 0 && fresh < g.pool_pages;
+  const int last = rest > 0 ? parent_row[full] : -1;
+  const bool last_ok = last >= 0 && last < g.pool_pages;
   if (layer == 0 && A.write_table) {
     int32_t* row = A.child_table + (int64_t)child * A.child_stride;
     for (int i = blockIdx.x * kThreads + threadIdx.x; i < A.child_stride; i += gridDim.x * kThreads) {
@@ -34,15 +36,14 @@ fork_kernel(const __grid_constant__ CacheSeqs cs, const CacheGeom g, const __gri
           page = -1;
         }
       } else if (i == full && rest > 0) {
-        if (fresh_ok) page = fresh;
-        else report_error(status, CC_ERR_DEVICE_FLAG, 612);
+        if (fresh_ok && last_ok) page = fresh;     // (a page that receives nothing holds what its last owner left)
+        else if (!fresh_ok) report_error(status, CC_ERR_DEVICE_FLAG, 612);
       }
       row[i] = page;
     }
   }
   if (rest == 0) return;
-  const int last = parent_row[full];
-  if (last < 0 || last >= g.pool_pages) {
+  if (!last_ok) {
     if (threadIdx.x == 0) report_error(status, CC_ERR_DEVICE_FLAG, 613);
     return;
   }

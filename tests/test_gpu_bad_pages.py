@@ -145,3 +145,18 @@ def test_infinite_logits_alone_are_not_a_row_without_slots(new):
     _, out, lse = attend(ctx(), cache, 8, [new], q=q)
     assert ctx().poll() == 0
     assert out[:, :4].isnan().all() and torch.isfinite(out[:, 4:]).all() and torch.isfinite(lse[:, 4:]).all()
+
+
+@pytest.mark.parametrize("bad", [-1, 2 ** 31 - 1, "pool"])
+def test_forks_of_a_parent_without_its_last_page(bad):
+    """The child's fresh page receives nothing, so the child does not get it: its old rows belong to nobody."""
+    cache = Cache([20, 37], 2, 8, seed=4, spare=3, poison=False)
+    cache.table[0, 2] = cache.pool if bad == "pool" else bad
+    child = torch.full((2, 5), 55, dtype=torch.int32, device="cuda")
+    k0, v0 = cache.k.clone(), cache.v.clone()
+    cc.cc_fork_pages(ctx(), cache.desc(2), [cache.k], [cache.v], [0, 1], child, cache.free)
+    assert ctx().poll() == cc.CC_ERR_DEVICE_FLAG
+    assert child[0].tolist() == cache.table[0, :2].tolist() + [-1] * 3
+    assert child[1].tolist() == cache.table[1, :4].tolist() + [int(cache.free[1])]
+    rows = torch.arange(8, device="cuda") + cache.free[0].long() * 8
+    assert torch.equal(cache.k[rows], k0[rows]) and torch.equal(cache.v[rows], v0[rows])
