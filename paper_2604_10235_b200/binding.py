@@ -415,6 +415,16 @@ def _raw_on(ctx: "Context", stream: Optional[int]) -> int:
     return torch.cuda.current_stream(ctx.device).cuda_stream if _CURRENT_RAW is None else _CURRENT_RAW(ctx.device)
 
 
+def _own_ws(ctx: "Context", stream: Optional[int], make) -> torch.Tensor:
+    """``make()``, a workspace that its call drops, allocated for the stream that the call runs on: torch's allocator then gives
+    the memory to later work of that stream only, and takes it from earlier work of that stream only."""
+    if stream is None:
+        return make()
+    # (1 is CUDA's other handle of the default stream, which torch does not know)
+    with torch.cuda.stream(torch.cuda.ExternalStream(0 if stream == 1 else stream, device=ctx.device)):
+        return make()
+
+
 def _stream(stream: Optional[int]) -> C.c_void_p:
     return C.c_void_p(_raw(stream))
 
@@ -428,7 +438,7 @@ def _ptr(t: Optional[torch.Tensor]) -> C.c_void_p:
 
 
 def cc_score_window(ctx: Context, desc: Desc, q_win, k, scores, lse=None, ws=None, stream=None):
-    ws = ctx.workspace(desc, 1) if ws is None else ws
+    ws = _own_ws(ctx, stream, lambda: ctx.workspace(desc, 1)) if ws is None else ws
     ctx.call("cc_score_window", desc, q_win, k, scores, lse, ws, _raw(stream))
 
 
@@ -437,7 +447,7 @@ def cc_fuse_prior_pool(ctx: Context, desc: Desc, scores, prior, fused, stream=No
 
 
 def cc_topk_select(ctx: Context, desc: Desc, fused, prior, idx, count, ws=None, stream=None):
-    ws = ctx.workspace(desc, 1) if ws is None else ws
+    ws = _own_ws(ctx, stream, lambda: ctx.workspace(desc, 1)) if ws is None else ws
     ctx.call("cc_topk_select", desc, fused, prior, idx, count, ws, _raw(stream))
 
 
@@ -523,7 +533,7 @@ def cc_select_spans(starts, ends, scores, protected, n: int, budget: int, span_r
 
 def cc_compress_layer(ctx: Context, desc: Desc, q_win, k, v, prior, k_out, v_out, idx, count,
                       free_pages=None, out_page_table=None, ws=None, stream=None):
-    ws = ctx.workspace(desc, 1) if ws is None else ws
+    ws = _own_ws(ctx, stream, lambda: ctx.workspace(desc, 1)) if ws is None else ws
     ctx.call("cc_compress_layer", desc, q_win, k, v, prior, k_out, v_out, idx, count, free_pages,
              out_page_table, ws, _raw(stream))
 
@@ -541,7 +551,7 @@ def cc_compress_layers(ctx: Context, desc: Desc, q_win, k, v, prior, k_out, v_ou
     """cc_compress_layer for a list of layers in one call: every tensor argument except ``prior``
     and ``ws`` is a list with one tensor per layer.  Layers may share buffers (an ``idx`` scratch, say);
     they then run one after the other instead of several to a launch."""
-    ws = ctx.workspace(desc, len(k)) if ws is None else ws
+    ws = _own_ws(ctx, stream, lambda: ctx.workspace(desc, len(k))) if ws is None else ws
     ctx.call("cc_compress_layers", desc, len(k), q_win, k, v, prior, k_out, v_out, idx, count, free_pages,
              out_page_table, ws, _raw(stream))
 
@@ -566,7 +576,7 @@ def cc_rope_append(ctx: Context, desc: CacheDesc, q_new, k_new, v_new, positions
 
 def cc_paged_attention(ctx: Context, desc: CacheDesc, q, k, v, out, lse=None, ws=None, stream=None):
     """Attention of the new tokens over the cache into ``out`` (and ``lse``)."""
-    ws = ctx.cache_workspace(desc) if ws is None else ws
+    ws = _own_ws(ctx, stream, lambda: ctx.cache_workspace(desc)) if ws is None else ws
     ctx.call_cache("cc_paged_attention", desc, q, k, v, out, lse, ws, _raw_on(ctx, stream))
 
 
