@@ -98,7 +98,7 @@ _SPEC = {"cc_score_window": b"iittttwi", "cc_fuse_prior_pool": b"iittti", "cc_to
          "cc_topk_select_static": b"iitttti", "cc_compact_kv": b"iippttttti",
          "cc_compress_layer": b"iittptttttttwi", "cc_compress_layers": b"iiiLLLtLLLLLLwi",
          "cc_ppl_chunk_scores": b"itiiiiiittti", "cc_select_chunks": b"itiiti",
-         "cc_rope_append": b"iidbbbnbbbi", "cc_paged_attention": b"iidbbbbfwi", "cc_fork_pages": b"iidiMMhinini"}
+         "cc_rope_append": b"iidbbbnbbbi", "cc_paged_attention": b"iidbbbbfWi", "cc_fork_pages": b"iidiMMhinini"}
 
 
 def load_library(path: Optional[str] = None) -> C.CDLL:

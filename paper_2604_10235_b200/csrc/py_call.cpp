@@ -12,6 +12,7 @@
 //   d  a device number (no word): the tensors of the kinds below are on that device
 //   b        a CUDA tensor of bfloat16, or None
 //   n, f     a contiguous CUDA tensor of int32, float32, or None
+//   W        a contiguous CUDA tensor as two words: address, number of elements; None: two zeros
 //   M  a sequence of bfloat16 tensors as a host array of addresses
 //   h  a contiguous host array (numpy) of 32-bit integers
 #define PY_SSIZE_T_CLEAN
@@ -93,6 +94,22 @@ bool typed_word(PyObject* o, PyObject* dtype, long device, bool none_ok, bool co
   return word_from(o, s_data_ptr, out);
 }
 
+bool workspace_words(PyObject* o, long device, uint64_t* out) {
+  out[0] = out[1] = 0;
+  if (o == Py_None) return true;
+  uint64_t at = 0;
+  if (!word_from(o, s_get_device, &at)) return false;
+  if ((long)at != device) {
+    PyErr_Format(PyExc_ValueError, "libcodecomp takes a workspace on cuda:%ld here", device);
+    return false;
+  }
+  if (!is_true(PyObject_CallMethodNoArgs(o, s_is_contiguous))) {
+    if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "libcodecomp takes a contiguous workspace");
+    return false;
+  }
+  return word_from(o, s_data_ptr, &out[0]) && word_from(o, s_numel, &out[1]);
+}
+
 bool host_word(PyObject* o, uint64_t* out) {
   Py_buffer view;
   if (PyObject_GetBuffer(o, &view, PyBUF_C_CONTIGUOUS) != 0) return false;
@@ -160,6 +177,7 @@ PyObject* call_bound(PyObject* self, PyObject* const* args, Py_ssize_t n_args) {
       case 't': ok = tensor_word(o, false, &a[n++]); break;
       case 'p': ok = tensor_word(o, true, &a[n++]); break;
       case 'w': ok = tensor_word(o, false, &a[n]) && word_from(o, s_numel, &a[n + 1]); n += 2; break;
+      case 'W': ok = workspace_words(o, device, &a[n]); n += 2; break;
       case 'd':
         device = PyLong_AsLong(o);
         ok = !(device == -1 && PyErr_Occurred());
@@ -217,8 +235,8 @@ PyObject* bind(PyObject*, PyObject* args) {
   if (len > kMaxWords) return PyErr_Format(PyExc_ValueError, "the spec of %s is too long", name);
   int words = 0;
   for (Py_ssize_t i = 0; i < len; ++i) {
-    if (!spec[i] || !strchr("itpwLdbnfMh", spec[i])) return PyErr_Format(PyExc_ValueError, "unknown kind of argument in the spec of %s", name);
-    words += spec[i] == 'w' ? 2 : spec[i] == 'd' ? 0 : 1;
+    if (!spec[i] || !strchr("itpwWLdbnfMh", spec[i])) return PyErr_Format(PyExc_ValueError, "unknown kind of argument in the spec of %s", name);
+    words += spec[i] == 'w' || spec[i] == 'W' ? 2 : spec[i] == 'd' ? 0 : 1;
     if (strchr("bnfM", spec[i]) && !t_f32) {
       PyObject* torch = PyImport_ImportModule("torch");
       if (!torch) return nullptr;
