@@ -98,7 +98,7 @@ _SPEC = {"cc_score_window": b"iittttwi", "cc_fuse_prior_pool": b"iittti", "cc_to
          "cc_topk_select_static": b"iitttti", "cc_compact_kv": b"iippttttti",
          "cc_compress_layer": b"iittptttttttwi", "cc_compress_layers": b"iiiLLLtLLLLLLwi",
          "cc_ppl_chunk_scores": b"itiiiiiittti", "cc_select_chunks": b"itiiti",
-         "cc_rope_append": b"iidbbbnbbbi", "cc_paged_attention": b"iidbbbbfWi", "cc_fork_pages": b"iidiMMhinini"}
+         "cc_rope_append": b"iidABBPCKKi", "cc_paged_attention": b"iidCKKOSWi", "cc_fork_pages": b"iidiMMhinini"}
 
 
 def load_library(path: Optional[str] = None) -> C.CDLL:
@@ -344,7 +344,8 @@ class RopePlan:
 class CacheDesc:
     """A ``cc_cache_desc`` plus the arrays it points to (kept alive here).  ``kv_lens``: tokens of each sequence in the
     cache, new ones included; ``new_lens``: new tokens of each (None: one each).  Strides are (token, head) pairs in
-    elements, None = dense."""
+    elements, None = dense: the tensor then has to be contiguous.  A tensor whose memory ends before its last row and head
+    is refused."""
 
     def __init__(self, n_heads_q: int, n_heads_kv: int, kv_lens: Sequence[int], new_lens: Optional[Sequence[int]] = None,
                  *, page_size: int, page_table: torch.Tensor, pool_pages: int, head_dim: int = 128,

@@ -10,11 +10,18 @@
 //   w  a CUDA tensor as two words: address, number of elements
 //   L  a sequence of tensors as a host array of addresses, or None
 //   d  a device number (no word): the tensors of the kinds below are on that device
-//   b        a CUDA tensor of bfloat16, or None
-//   n, f     a contiguous CUDA tensor of int32, float32, or None
-//   W        a contiguous CUDA tensor as two words: address, number of elements; None: two zeros
-//   M  a sequence of bfloat16 tensors as a host array of addresses
+//   n  a contiguous CUDA tensor of int32, or None
+//   W  a contiguous CUDA tensor as two words: address, number of elements; None: two zeros
 //   h  a contiguous host array (numpy) of 32-bit integers
+// and, where the second argument is a cc_cache_desc, tensors that hold what it describes, or None:
+//   A  q_new      B  k_new, v_new      C  q      K  k, v      O  out         bfloat16
+//   P  positions (int32), S  lse (float32)                                   contiguous
+//   M  a sequence of k or v (none of them None) as a host array of addresses
+// A tensor for which the descriptor gives no strides has to be contiguous; the memory from a tensor's first element to
+// its last one has to hold all rows and heads at the descriptor's strides, whatever the shape in which it comes.
+//
+// What a torch.Tensor is and where it lies comes from torch's DLPack table in one call, where this torch has one: the eight tensors of a
+// rotation take 0.8 us with all checks; by their methods, and without the checks of sizes and strides, they took 2.9.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <stdint.h>
@@ -31,8 +38,10 @@ namespace {
 
 constexpr int kMaxWords = 20;
 
-PyObject *s_data_ptr, *s_is_cuda, *s_is_pinned, *s_numel, *s_dtype, *s_get_device, *s_is_contiguous;
+PyObject *s_data_ptr, *s_is_cuda, *s_is_pinned, *s_numel, *s_dtype, *s_get_device, *s_shape, *s_stride;
 PyObject *t_bf16, *t_i32, *t_f32;      // torch's types, looked up with the first spec that names one
+const char kTyped[] = "nABCKOPSM";     // kinds whose type and device are checked
+const char kLaidOut[] = "ABCKOPSM";    // of them those that the descriptor lays out
 
 bool word_of(PyObject* o, uint64_t* out) {
   *out = PyLong_AsUnsignedLongLongMask(o);
@@ -71,43 +80,186 @@ bool tensor_word(PyObject* o, bool pinned_ok, uint64_t* out) {
   return word_from(o, s_data_ptr, out);
 }
 
-// A tensor of the given type on the given device, or None where that is allowed.
-bool typed_word(PyObject* o, PyObject* dtype, long device, bool none_ok, bool contiguous, uint64_t* out) {
-  if (none_ok && o == Py_None) {
-    *out = 0;
-    return true;
+// What the checks need of a tensor.
+struct Tensor {
+  PyObject* dtype;             // borrowed
+  long device;                 // -1: the host
+  uint64_t address;
+  bool contiguous;
+  int64_t reach;               // elements from the first one to the last one
+};
+
+// From the sizes and strides, innermost last.
+template <class Dim>
+void lay_out(Py_ssize_t dims, const Dim& dim, Tensor* t) {
+  int64_t dense = 1, last = 0;
+  bool none = false;
+  t->contiguous = true;
+  for (Py_ssize_t i = dims - 1; i >= 0; --i) {
+    const std::pair<int64_t, int64_t> d = dim(i);          // size, stride
+    none |= d.first == 0;
+    if (d.first == 1) continue;
+    t->contiguous &= d.second == dense;
+    dense *= d.first;
+    last += (d.first - 1) * d.second;
   }
-  PyObject* t = PyObject_GetAttr(o, s_dtype);
-  if (!t) return false;
-  const bool same = t == dtype;
-  Py_DECREF(t);
+  t->contiguous |= none;
+  t->reach = none ? 0 : last + 1;
+}
+
+// By the object's own methods (a subclass of torch.Tensor, or whatever else behaves like one).
+bool describe_by_methods(PyObject* o, Tensor* t) {
   uint64_t at = 0;
-  if (same && !word_from(o, s_get_device, &at)) return false;
-  if (!same || (long)at != device) {
+  t->dtype = PyObject_GetAttr(o, s_dtype);
+  if (!t->dtype) return false;
+  Py_DECREF(t->dtype);                                     // (torch keeps its types)
+  if (!word_from(o, s_get_device, &at) || !word_from(o, s_data_ptr, &t->address)) return false;
+  t->device = (long)at;
+  PyObject* shape = PyObject_GetAttr(o, s_shape);
+  PyObject* stride = shape ? PyObject_CallMethodNoArgs(o, s_stride) : nullptr;
+  bool ok = stride && PyTuple_Check(shape) && PyTuple_Check(stride) && PyTuple_GET_SIZE(shape) == PyTuple_GET_SIZE(stride);
+  if (ok)
+    lay_out(PyTuple_GET_SIZE(shape), [&](Py_ssize_t i) {
+      return std::make_pair((int64_t)PyLong_AsLongLong(PyTuple_GET_ITEM(shape, i)), (int64_t)PyLong_AsLongLong(PyTuple_GET_ITEM(stride, i)));
+    }, t);
+  Py_XDECREF(shape);
+  Py_XDECREF(stride);
+  if (!ok && !PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "a tensor is needed");
+  return ok && !PyErr_Occurred();
+}
+
+// The C interface of DLPack 1.3 and later 1.x, as far as it is used: what a tensor is, without a reference to it.
+struct DlTensor {
+  void* data;
+  struct { int32_t type, id; } device;                     // type 2: CUDA
+  int32_t dims;
+  struct { uint8_t code, bits; uint16_t lanes; } dtype;    // code 0: integers, 2: floats, 4: bfloat
+  int64_t *shape, *strides;
+  uint64_t byte_offset;
+};
+struct DlTable {
+  uint32_t major, minor;
+  void *older, *allocate, *to_managed, *from_managed;
+  int (*describe)(void* object, DlTensor* out);
+};
+const DlTable* g_table;        // of torch.Tensor, or null: a torch without one
+PyTypeObject* g_tensor;
+
+void find_table(PyObject* torch) {
+  PyObject* type = PyObject_GetAttrString(torch, "Tensor");
+  PyObject* capsule = type ? PyObject_GetAttrString(type, "__dlpack_c_exchange_api__") : nullptr;
+  const DlTable* table = capsule ? static_cast<const DlTable*>(PyCapsule_GetPointer(capsule, "dlpack_exchange_api")) : nullptr;
+  if (table && table->major == 1 && table->minor >= 3 && table->describe) {
+    g_table = table;                   // (alive as long as the process)
+    g_tensor = reinterpret_cast<PyTypeObject*>(type);
+    Py_INCREF(type);
+  }
+  Py_XDECREF(capsule);
+  Py_XDECREF(type);
+  PyErr_Clear();
+}
+
+bool describe_by_table(PyObject* o, Tensor* t) {
+  DlTensor d;
+  if (g_table->describe(o, &d) != 0) {
+    if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "a tensor that DLPack cannot describe");
+    return false;
+  }
+  const auto is = [&](int code, int bits) { return d.dtype.code == code && d.dtype.bits == bits && d.dtype.lanes == 1; };
+  t->dtype = is(4, 16) ? t_bf16 : is(2, 32) ? t_f32 : is(0, 32) ? t_i32 : nullptr;
+  t->device = d.device.type == 2 ? d.device.id : -1;
+  t->address = (uint64_t)(uintptr_t)d.data + d.byte_offset;
+  lay_out(d.dims, [&](Py_ssize_t i) { return std::make_pair(d.shape[i], d.strides[i]); }, t);
+  return true;
+}
+
+bool describe(PyObject* o, Tensor* t) {
+  return g_table && Py_TYPE(o) == g_tensor ? describe_by_table(o, t) : describe_by_methods(o, t);
+}
+
+// A tensor of the given type on the given device.
+bool typed(PyObject* o, PyObject* dtype, long device, bool contiguous, Tensor* t) {
+  if (!describe(o, t)) return false;
+  if (t->dtype != dtype || t->device != device) {
     PyErr_Format(PyExc_ValueError, "libcodecomp takes a tensor of %S on cuda:%ld here", dtype, device);
     return false;
   }
-  if (contiguous && !is_true(PyObject_CallMethodNoArgs(o, s_is_contiguous))) {
-    if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "libcodecomp takes a contiguous tensor here");
+  if (contiguous && !t->contiguous) {
+    PyErr_SetString(PyExc_ValueError, "libcodecomp takes a contiguous tensor here");
     return false;
   }
-  return word_from(o, s_data_ptr, out);
+  return true;
 }
 
 bool workspace_words(PyObject* o, long device, uint64_t* out) {
-  out[0] = out[1] = 0;
-  if (o == Py_None) return true;
-  uint64_t at = 0;
-  if (!word_from(o, s_get_device, &at)) return false;
-  if ((long)at != device) {
-    PyErr_Format(PyExc_ValueError, "libcodecomp takes a workspace on cuda:%ld here", device);
+  Tensor t = {};
+  if (o != Py_None) {
+    if (!describe(o, &t)) return false;
+    if (t.device != device || !t.contiguous) {
+      PyErr_Format(PyExc_ValueError, "libcodecomp takes a contiguous workspace on cuda:%ld here", device);
+      return false;
+    }
+  }
+  out[0] = t.address;
+  out[1] = (uint64_t)t.reach;
+  return true;
+}
+
+PyObject* dtype_of(char kind) { return kind == 'n' || kind == 'P' ? t_i32 : kind == 'S' ? t_f32 : t_bf16; }
+
+// New tokens of all sequences; -1: a descriptor that the call refuses.
+int64_t new_tokens(const cc_cache_desc* d) {
+  if (!d || d->num_seqs < 1 || d->num_seqs > CC_MAX_SEQS) return -1;
+  if (!d->new_lens) return d->num_seqs;
+  int64_t tokens = 0;
+  for (int s = 0; s < d->num_seqs; ++s) {
+    if (d->new_lens[s] < 0) return -1;
+    tokens += d->new_lens[s];
+  }
+  return tokens;
+}
+// Elements that a tensor of the kind reaches over, by the descriptor; whether it has to be contiguous.  False: nothing to check (no work, or
+// a descriptor that the call refuses).
+struct Wanted {
+  __int128 reach;
+  bool dense;
+};
+bool wanted(const cc_cache_desc* d, int64_t tokens, char kind, Wanted* w) {
+  if (tokens < 0 || d->n_heads_q < 1 || d->n_heads_kv < 1 || (tokens == 0 && kind != 'M')) return false;
+  const bool pool = kind == 'K' || kind == 'M';
+  if (pool && (d->pool_pages < 1 || d->page_size < 1)) return false;
+  const __int128 rows = pool ? (__int128)d->pool_pages * d->page_size : tokens;
+  if (kind == 'P' || kind == 'S') {
+    *w = {rows * (kind == 'S' ? d->n_heads_q : 1), true};
+    return true;
+  }
+  const int64_t heads = kind == 'B' || pool ? d->n_heads_kv : d->n_heads_q;
+  int64_t tok = pool ? d->kv_stride_tok : kind == 'A' ? d->q_new_stride_tok : kind == 'B' ? d->kv_new_stride_tok
+                : kind == 'C' ? d->q_stride_tok : d->out_stride_tok;
+  int64_t head = pool ? d->kv_stride_head : kind == 'A' ? d->q_new_stride_head : kind == 'B' ? d->kv_new_stride_head
+                 : kind == 'C' ? d->q_stride_head : d->out_stride_head;
+  if (tok < 0 || head < 0) return false;
+  w->dense = tok == 0 && head == 0;
+  if (tok == 0) tok = heads * d->head_dim;
+  if (head == 0) head = d->head_dim;
+  w->reach = (rows - 1) * tok + (__int128)(heads - 1) * head + d->head_dim;
+  return true;
+}
+
+bool holds(const Tensor& t, const cc_cache_desc* d, int64_t tokens, char kind, const char* name) {
+  Wanted w;
+  if (!wanted(d, tokens, kind, &w)) return true;
+  const char* what = kind == 'A' ? "q_new" : kind == 'B' ? "k_new or v_new" : kind == 'C' ? "q" : kind == 'O' ? "out"
+                     : kind == 'P' ? "positions" : kind == 'S' ? "lse" : "k or v";
+  if (w.dense && !t.contiguous) {
+    PyErr_Format(PyExc_ValueError, "%s: the descriptor gives no strides for %s, which is not contiguous", name, what);
     return false;
   }
-  if (!is_true(PyObject_CallMethodNoArgs(o, s_is_contiguous))) {
-    if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "libcodecomp takes a contiguous workspace");
+  if (w.reach > t.reach) {
+    PyErr_Format(PyExc_ValueError, "%s: %s reaches over %lld elements, fewer than the descriptor describes", name, what, (long long)t.reach);
     return false;
   }
-  return word_from(o, s_data_ptr, &out[0]) && word_from(o, s_numel, &out[1]);
+  return true;
 }
 
 bool host_word(PyObject* o, uint64_t* out) {
@@ -167,6 +319,8 @@ PyObject* call_bound(PyObject* self, PyObject* const* args, Py_ssize_t n_args) {
   }
   uint64_t a[kMaxWords];
   std::vector<std::vector<uint64_t>> lists;      // host arrays of the call (moving the outer one keeps their storage)
+  struct Laid { char kind; Tensor t; };
+  std::vector<Laid> laid;                        // checked when the type of every argument is
   int n = 0;
   long device = -1;
   for (Py_ssize_t i = 0; i < n_args; ++i) {
@@ -182,10 +336,19 @@ PyObject* call_bound(PyObject* self, PyObject* const* args, Py_ssize_t n_args) {
         device = PyLong_AsLong(o);
         ok = !(device == -1 && PyErr_Occurred());
         break;
-      case 'b': ok = typed_word(o, t_bf16, device, true, false, &a[n++]); break;
-      case 'n': ok = typed_word(o, t_i32, device, true, true, &a[n++]); break;
-      case 'f': ok = typed_word(o, t_f32, device, true, true, &a[n++]); break;
       case 'h': ok = host_word(o, &a[n++]); break;
+      case 'n':
+      case 'A': case 'B': case 'C': case 'K': case 'O': case 'P': case 'S': {
+        const char kind = f->spec[i];
+        Tensor t = {};
+        if (o != Py_None) ok = typed(o, dtype_of(kind), device, strchr("nPS", kind), &t);
+        a[n++] = t.address;
+        if (ok && o != Py_None && kind != 'n') {
+          if (laid.empty()) laid.reserve(8);
+          laid.push_back({kind, t});
+        }
+        break;
+      }
       case 'M':
       case 'L': {
         if (o == Py_None && f->spec[i] == 'L') { a[n++] = 0; break; }
@@ -195,8 +358,14 @@ PyObject* call_bound(PyObject* self, PyObject* const* args, Py_ssize_t n_args) {
         lists.emplace_back((size_t)m + 1);
         for (Py_ssize_t j = 0; j < m && ok; ++j) {
           PyObject* item = PySequence_Fast_GET_ITEM(seq, j);
-          ok = f->spec[i] == 'L' ? word_from(item, s_data_ptr, &lists.back()[j])
-                                 : typed_word(item, t_bf16, device, false, false, &lists.back()[j]);
+          if (f->spec[i] == 'L') {
+            ok = word_from(item, s_data_ptr, &lists.back()[j]);
+            continue;
+          }
+          Tensor t = {};
+          ok = typed(item, t_bf16, device, false, &t);
+          lists.back()[j] = t.address;
+          if (ok) laid.push_back({'M', t});
         }
         Py_DECREF(seq);
         a[n++] = (uint64_t)(uintptr_t)lists.back().data();
@@ -204,6 +373,12 @@ PyObject* call_bound(PyObject* self, PyObject* const* args, Py_ssize_t n_args) {
       }
     }
     if (!ok) return nullptr;
+  }
+  if (!laid.empty()) {
+    const cc_cache_desc* desc = reinterpret_cast<const cc_cache_desc*>((uintptr_t)a[1]);
+    const int64_t tokens = new_tokens(desc);
+    for (const Laid& x : laid)
+      if (!holds(x.t, desc, tokens, x.kind, f->entry->name)) return nullptr;
   }
   int rc;
   Py_BEGIN_ALLOW_THREADS
@@ -235,18 +410,21 @@ PyObject* bind(PyObject*, PyObject* args) {
   if (len > kMaxWords) return PyErr_Format(PyExc_ValueError, "the spec of %s is too long", name);
   int words = 0;
   for (Py_ssize_t i = 0; i < len; ++i) {
-    if (!spec[i] || !strchr("itpwWLdbnfMh", spec[i])) return PyErr_Format(PyExc_ValueError, "unknown kind of argument in the spec of %s", name);
+    if (!spec[i] || !strchr("itpwWLdnhABCKOPSM", spec[i])) return PyErr_Format(PyExc_ValueError, "unknown kind of argument in the spec of %s", name);
     words += spec[i] == 'w' || spec[i] == 'W' ? 2 : spec[i] == 'd' ? 0 : 1;
-    if (strchr("bnfM", spec[i]) && !t_f32) {
+    if (strchr(kTyped, spec[i]) && !t_f32) {
       PyObject* torch = PyImport_ImportModule("torch");
       if (!torch) return nullptr;
       t_bf16 = PyObject_GetAttrString(torch, "bfloat16");
       t_i32 = PyObject_GetAttrString(torch, "int32");
       t_f32 = PyObject_GetAttrString(torch, "float32");
+      find_table(torch);
       Py_DECREF(torch);
       if (!t_bf16 || !t_i32 || !t_f32) return nullptr;
     }
   }
+  if (strpbrk(spec, kLaidOut) && strncmp(spec, "iid", 3) != 0)
+    return PyErr_Format(PyExc_ValueError, "the spec of %s has no descriptor", name);
   if (words != entry->words) return PyErr_Format(PyExc_ValueError, "%s takes %d words, its spec gives %d", name, entry->words, words);
   Bound* f = new (std::nothrow) Bound{entry, reinterpret_cast<void*>((uintptr_t)fn), (int)len, {}};
   if (!f) return PyErr_NoMemory();
@@ -275,6 +453,7 @@ PyMODINIT_FUNC PyInit__cccall(void) {
   s_numel = PyUnicode_InternFromString("numel");
   s_dtype = PyUnicode_InternFromString("dtype");
   s_get_device = PyUnicode_InternFromString("get_device");
-  s_is_contiguous = PyUnicode_InternFromString("is_contiguous");
+  s_shape = PyUnicode_InternFromString("shape");
+  s_stride = PyUnicode_InternFromString("stride");
   return PyModule_Create(&module);
 }
