@@ -287,6 +287,10 @@ int cc_select_chunks(cc_ctx* ctx, const float* score, int32_t num_chunks, int32_
  * bound of each, so that a captured graph can be replayed while its sequences grow; a value outside
  * [0, kv_lens[s]] is clamped and flagged.  Work is shared out by the lengths found.
  *
+ * Limits.  At most 128 query heads per KV head, 2^30 tokens of a sequence and 2^30 new ones of a call, CC_MAX_SEQS
+ * sequences, a pool of less than 2^31 rows, CC_MAX_CHILDREN children; strides are multiples of 8 elements up to 2^32,
+ * pointers on 16-byte boundaries.
+ *
  * These calls run on the context's device, whichever is current.  Calls whose work may overlap on the GPU (streams,
  * captured graphs) need workspaces of their own. */
 
@@ -361,7 +365,8 @@ size_t cc_attention_workspace_bytes(const cc_ctx* ctx, const cc_cache_desc* desc
  * h / (H_q / H_kv), over the slots j that it attends to (all, or those up to n_s - T_s + t):
  *   out = sum_j softmax_j(scale * q . k_j) v_j,   lse = log sum_j exp(scale * q . k_j).
  * A token that attends to no slot (none, or slots on missing pages alone) gets out = 0 and lse = -inf.  lse may be
- * NULL.  bf16 operands, f32 products, sums and softmax, probabilities rounded to bf16 for the product with v, one
+ * NULL.  bf16 operands, f32 products, sums and softmax (of more than 16 rows per sequence and KV head some
+ * exponentials are good to 8e-5, the others to 2^-22), probabilities rounded to bf16 for the product with v, one
  * rounding of the result.  Rows of k and v beyond n_s are never used, whatever they hold.  out must not overlap q, k
  * or v. */
 int cc_paged_attention(cc_ctx* ctx, const cc_cache_desc* desc, const void* q, const void* k,

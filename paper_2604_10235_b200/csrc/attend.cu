@@ -152,7 +152,7 @@ attend_join_few_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as,
 }
 
 // Many parts of few problems: a block takes four rows of a problem, eight lanes a row, each of its warps every eighth part (38 tokens
-// over 18246 keys, 2 KV heads: 30.6 -> 20.2 us).  Every block looks through all places, so it loses where there are many of
+// over 18246 keys, 2 KV heads: 30.6 -> 19.9 us).  Every block looks through all places, so it loses where there are many of
 // them: 219 tokens in two sequences, 28 problems of 256 rows in five parts, 26.7 -> 36.9 us.
 __global__ void __launch_bounds__(kJoinWarps * 32)
 attend_join_spread_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as, const AttendWs ws, int grid, const AttendOut o,
@@ -235,7 +235,7 @@ attend_join_spread_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs 
 }
 
 // Many rows of a few parts: eight lanes take a row, all of them two parts at once, so that a warp does four rows in the time of one (a
-// warp per row and four rows after one another: 15 us of the 90 of 517 tokens over 8709 keys).
+// warp per row and four rows after one another took 15 us for 517 tokens over 8709 keys, this takes about 7).
 __global__ void __launch_bounds__(kJoinWarps * 32)
 attend_join_kernel(const CacheGeom g, const __grid_constant__ AttendSeqs as, const AttendWs ws, int grid, const AttendOut o,
                    DeviceStatus* status) {
@@ -347,8 +347,8 @@ AttendPlans plan_attend(const CacheSeqs& cs, const CacheGeom& g, int sm_count) {
   many.block_tokens = 2 * many.tile_tokens;
   many.start_weight = 3;              // (2: ragged chunks 273 -> 254 us with 3; 4: 257)
   // A batch of both kinds goes to the tensor-core kernel as a whole unless the sequences with few rows have many keys: that kernel
-  // takes a quarter longer over them (64 tokens over 245000 keys x 8 heads: 213 against 168 us) and a launch of their own costs
-  // 10 us (16 sequences of 1 to 8 tokens, four of them with few rows: 58.6 against 48.7 us).
+  // takes a quarter longer over them (64 tokens over 245000 keys x 8 heads: 201 against 163 us) and a launch of their own costs
+  // 14 us (16 sequences of 1 to 8 tokens, four of them with few rows: 59.4 against 45.2 us).
   int64_t few_keys = 0;
   bool mixed = false;
   auto is_few = [&](int T) { return (int64_t)T * g.group <= kRowsMost; };

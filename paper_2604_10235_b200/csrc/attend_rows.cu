@@ -3,17 +3,17 @@
 //   o_r = sum_j p_rj v_j / sum_j p_rj,   p_rj = exp(scale q_r . k_j - reference_r)
 //
 // Every row of K and V is read once and 4 flops are done with each of its bytes per query row: bound by HBM (64 sequences, 245 k
-// keys, 8 heads, 1.0 GB: 156 to 165 us, 6.1 to 6.4 TB/s), few keys by latency (2305 keys x 8 heads 10.0 to 11.0 us, of which the kernel 5).  The matrix
+// keys, 8 heads, 1.0 GB: 157 to 164 us, 6.1 to 6.4 TB/s), few keys by latency (2305 keys x 8 heads 9.8 to 10.3 us, of which the kernel 5).  The matrix
 // instructions are mma.sync (m16n8k16): the 16 rows are their M side, against at least 64 of tcgen05.mma, and a tile's 32 per
 // scheduler, some 500 clocks, fit well into the 1400 that its 32 KB take at this SM's share of the bandwidth.  The tensor-core
-// kernel takes 213 us for the same.
+// kernel takes 201 us for the same.
 //
 // One CTA per SM.  A warp brings K and V tiles of 64 keys by TMA, one copy per page, through a ring of four stages of 32 KB,
 // and the query rows of the next problem beside them; eight warps work on them in two groups that take tiles by turns, a
 // warp on 16 keys of a tile.  Each warp has a running reference, sum and output of its own for all rows, so that
 // tiles need no exchange between warps; they meet once per problem, each leaving its output in shared memory, where all threads
-// add them up (one barrier; added by halves with three: 162 us).  A reference is replaced only when a logit exceeds it by 2^8:
-// outputs are sums in f32, and a probability of up to 2^8 rounds to bf16 like any other.
+// add them up (one barrier; added by halves with three: 162 us).  A reference is replaced only when a logit, in units of
+// log2, exceeds it by 8: outputs are sums in f32, and a probability of up to 2^8 rounds to bf16 like any other.
 #include <cuda_bf16.h>
 
 #include "attend_plan.cuh"

@@ -14,8 +14,9 @@
 // P up to 1.  So only tiles with masked keys look at their maximum beforehand, the others compute with the reference that there is
 // (of a row's first keys); where the sum of a half tile shows that a logit is far above it (or no number), nothing has been
 // handed over yet, the row's maximum becomes the reference, its O is scaled in tensor memory and the half is computed again.
-// One pair of exponentials in eight is evaluated on the FMA pipe (exp2_poly.cuh): 2048 x 32768 1057 us with one in four, 1054 with one in
-// eight, 1077 with one in sixteen; 517 x 8709 96.3, 94.1, 94.7.
+// One pair of exponentials in eight is evaluated on the FMA pipe (exp2_poly.cuh, good to 7.8e-5, a fiftieth of what P loses as bf16): 517
+// tokens over 8709 keys take 79.6 us with one pair in four, 77.7 with one in eight, 77.3 with one in sixteen; 2048 over 32768, at
+// the power limit, 1042, 1058 and 1054, within what two runs differ by.
 //
 // Roles (320 threads, one CTA per SM): warps 0-3 and 4-7 the softmax of the two tiles, warp 8 the copies (Q once per
 // problem, K and V by turns through a ring of five stages of 32 KB, a copy per page), warp 9 the products.

@@ -135,3 +135,16 @@ def test_tensors_that_require_gradients_are_tensors():
     t["q"].requires_grad_(True)
     t["k"] = torch.nn.Parameter(t["k"])
     assert invoke("attend", t) == cc.CC_ERR_INVALID_ARG
+
+
+def test_rows_of_a_descriptor():
+    class Table:
+        dtype, is_cuda, device, shape = torch.int32, True, "cuda:0", (3, 200)
+        is_contiguous = staticmethod(lambda: True)
+        dim = staticmethod(lambda: 2)
+        data_ptr = staticmethod(lambda: 4096)
+        get_device = staticmethod(lambda: 0)
+    more = dict(page_size=16, page_table=Table, pool_pages=9)
+    assert cc.CacheDesc(32, 8, [2065, 1233], [17, 1], **more).n_new == 18
+    d = cc.CacheDesc(32, 8, [5, 0, 7], **more)
+    assert d.n_new == 3 and d.lens == [5, 0, 7]
