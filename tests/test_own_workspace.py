@@ -132,3 +132,34 @@ def test_compression_on_a_busy_stream():
     assert all((x == 5).all() for x in after)
     for a, b in zip(want, got):
         assert torch.equal(a, b)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("new", [[1, 1], [40, 90]])
+def test_streams_by_handle(new):
+    """CUDA's handles of the default streams, and a stream that is being captured."""
+    from cache_util import D, Cache, assert_attention, attend_reference
+    from gpu_util import ctx as context
+    cache = Cache([9000, 3000], 4, 16, seed=9)
+    desc = cache.desc(16, new)
+    q = torch.randn((sum(new), 16, D), device="cuda").bfloat16()
+    ref = attend_reference(cache, q, new)
+    for handle in (0, 1, 2, torch.cuda.current_stream().cuda_stream):
+        out = torch.zeros_like(q)
+        torch.cuda.synchronize()
+        cc.cc_paged_attention(context(), desc, q, cache.k, cache.v, out, stream=handle)
+        torch.cuda.synchronize()
+        assert context().poll() == 0
+        assert_attention(out, None, ref)
+    out = torch.zeros_like(q)
+    side = torch.cuda.Stream()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        cc.cc_paged_attention(context(), desc, q, cache.k, cache.v, out, stream=side.cuda_stream)
+    for _ in range(3):
+        out.zero_()
+        x = [torch.full((1 << 20,), 5, dtype=torch.uint8, device="cuda") for _ in range(4)]
+        graph.replay()
+        torch.cuda.synchronize()
+        assert context().poll() == 0 and all((y == 5).all() for y in x)
+        assert_attention(out, None, ref)
